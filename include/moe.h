@@ -577,6 +577,112 @@ int moe_shared_expert_bwd(const moe_bf16* x, const moe_bf16* u_s, const moe_bf16
                           int32_t D, int32_t Fs, float* dx, int32_t accumulate_dx, float* dWs1,
                           float* dWs2, void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* ---------------------------------------------------------------------- */
+/* 8-bit integer weights and activations (serving).                        */
+/* A row x of activations, and an output channel of a weight, is held as    */
+/* integers q in [-127, 127] and one fp32 scale:                            */
+/*   scale = max|x| / 127,   q = 127 x / max|x| rounded to the nearest      */
+/*   integer, ties to even (exactly: no rounding but that one).             */
+/* A row of zeros has scale 0 and codes 0.  A row that holds an infinity or */
+/* a NaN has a NaN scale and codes 0, so every product with it is NaN.      */
+/* Products accumulate exactly in 32-bit integers.                          */
+/* ---------------------------------------------------------------------- */
+/* Rows of activations.
+ *   x [R, D] bf16;  q [R, D] int8 (16-byte aligned);  scale [R] fp32 */
+int moe_quant_rows_i8(const moe_bf16* x, int64_t R, int32_t D, int8_t* q, float* scale, hipStream_t stream);
+
+/* Weights, laid out once: their output channels become rows, so that a channel's
+ * contraction is contiguous.
+ *   W [E, Kd, N] bf16;  Wq [E, N, Kd] int8 (16-byte aligned);  scale [E, N] fp32
+ * (16-byte aligned, as the products below read it).  A single dense weight is E = 1.
+ * Errors (these and the products below): Kd a multiple of 16 in [16, 65536], N a
+ * multiple of 8 in [8, 65536], E in [1, 1024] (MOE_ERR_SHAPE); Kd*N*2 below
+ * 2^31 (MOE_ERR_UNSUPPORTED). */
+int moe_quant_weights_i8(const moe_bf16* W, int32_t E, int32_t Kd, int32_t N, int8_t* Wq, float* scale,
+                         hipStream_t stream);
+
+/* moe_grouped_gemm in 8-bit integers: for r in expert e's segment
+ *   v[r, n] = a_scale[r] * w_scale[e, n] * sum_k Aq[r, k] Wq[e, n, k]
+ *   epilogue 0: C = bf16(v);   epilogue 1: C = bf16(max(v, 0)^2)
+ *   Aq [R, Kd] int8 (16-byte aligned);  a_scale [R];  Wq [E, N, Kd];  w_scale [E, N];
+ *   C [R, N] bf16;  sched from moe_grouped_schedule for the same offsets, E and R,
+ *   or NULL with E = 1 for a dense product over all R rows. */
+int moe_grouped_gemm_i8(const int8_t* Aq, const float* a_scale, const void* sched, int32_t E, int64_t R,
+                        int32_t Kd, int32_t N, const int8_t* Wq, const float* w_scale, int32_t epilogue,
+                        moe_bf16* C, hipStream_t stream);
+
+/* Workspace bytes moe_latent_proj_i8 needs; 0 for invalid sizes. */
+size_t moe_latent_proj_i8_workspace_bytes(int64_t M, int32_t Kd);
+
+/* moe_latent_proj with an 8-bit weight: the rows of A are quantised, then
+ * C[m, n] = bf16(scale[m] * w_scale[n] * sum_k Aq[m, k] Wq[n, k]).
+ *   A [M, Kd] bf16;  Wq [N, Kd] int8;  w_scale [N];  C [M, N] bf16;  ws 256-byte aligned. */
+int moe_latent_proj_i8(const moe_bf16* A, const int8_t* Wq, const float* w_scale, int64_t M, int32_t Kd, int32_t N,
+                       moe_bf16* C, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Workspace bytes moe_grouped_ffn_i8 needs; 0 for invalid sizes. */
+size_t moe_grouped_ffn_i8_workspace_bytes(int32_t E, int64_t R, int32_t D, int32_t F);
+
+/* moe_grouped_ffn with 8-bit weights (inference only: nothing is saved for a
+ * backward pass).  Rows of x_disp are quantised;
+ *   h[r] = bf16(max(sx[r] * s1[e] * (xq[r] . W1q[e]), 0)^2), whose rows are quantised;
+ *   y_disp[r] = bf16(sh[r] * s2[e] * (hq[r] . W2q[e])).
+ *   x_disp [R, D] bf16;  offsets [E+1];  W1q [E, F, D], W2q [E, D, F] int8;
+ *   s1 [E, F], s2 [E, D];  y_disp [R, D] bf16;  ws 256-byte aligned.
+ * D and F multiples of 16. */
+int moe_grouped_ffn_i8(const moe_bf16* x_disp, const int32_t* offsets, int32_t E, int64_t R, int32_t D, int32_t F,
+                       const int8_t* W1q, const float* s1, const int8_t* W2q, const float* s2, moe_bf16* y_disp,
+                       void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------------------- */
+/* Whole layer forward for a few tokens (a decode step, drafted tokens).    */
+/* ---------------------------------------------------------------------- */
+#define MOE_FEW_MAX_TOKENS 64
+
+enum { MOE_WEIGHTS_BF16 = 0, MOE_WEIGHTS_I8 = 1 };
+
+typedef struct {
+    uint32_t struct_size;      /* sizeof(moe_layer_few_args) */
+    int64_t S;                 /* tokens, 0 .. MOE_FEW_MAX_TOKENS */
+    int32_t D, E, K, F;
+    int32_t Fs;                /* shared-expert width; 0 = none */
+    int32_t score_fn;          /* MOE_SCORE_SOFTMAX or MOE_SCORE_SIGMOID */
+    int32_t weights;           /* MOE_WEIGHTS_BF16 or MOE_WEIGHTS_I8, the shared expert's included */
+    const moe_bf16* x;         /* [S, D] */
+    const float* Wr;           /* [D, E] */
+    const float* router_bias;  /* [E] or NULL */
+    const float* sel_bias;     /* [E] selection-only bias (sigmoid scores only) or NULL */
+    const void* W1;            /* bf16 [E, D, F], or int8 [E, F, D] */
+    const void* W2;            /* bf16 [E, F, D], or int8 [E, D, F] */
+    const void* Ws1;           /* bf16 [D, Fs], or int8 [Fs, D]; NULL when Fs = 0 */
+    const void* Ws2;           /* bf16 [Fs, D], or int8 [D, Fs]; NULL when Fs = 0 */
+    const float* s1;           /* channel scales of 8-bit weights: [E, F] */
+    const float* s2;           /* [E, D] */
+    const float* ss1;          /* [Fs] */
+    const float* ss2;          /* [D]; all NULL with bf16 weights */
+    moe_bf16* y;               /* [S, D] */
+    int32_t* topk_idx;         /* [S, K] exported, or NULL */
+    float* topk_prob;          /* [S, K] exported, or NULL */
+    void* ws;                  /* 256-byte aligned, >= moe_layer_few_workspace_bytes */
+    size_t ws_bytes;
+} moe_layer_few_args;
+
+/* Workspace bytes for these sizes and modes (no pointer is read); 0 if they are
+ * invalid or S = 0. */
+size_t moe_layer_few_workspace_bytes(const moe_layer_few_args* a);
+
+/* y[t] = bf16( sum_k p[t,k] FFN_{T_k}(x[t]) [+ shared(x[t])] ): moe_layer_fwd's
+ * layer (no latent projection) for S <= 64 tokens, without a permutation.  Picks and
+ * weights follow moe_route_topk or moe_route_sigmoid on fp32-accurate logits; sums over
+ * the K experts and the shared expert are fp32 with one rounding, to y.  Expert
+ * activations are rounded to bf16 (and, with 8-bit weights, quantised as in
+ * moe_grouped_ffn_i8).  The logits' last bits may differ from moe_router_logits'.
+ * With 8-bit weights D, F and Fs are multiples of 16.
+ * Errors: MOE_ERR_SHAPE for sizes (S > MOE_FEW_MAX_TOKENS among them), unknown modes,
+ * sel_bias with softmax scores, and shared weights or scales where there are none to
+ * be; otherwise as moe_layer_fwd. */
+int moe_layer_few(const moe_layer_few_args* a, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -63,7 +63,20 @@ class LayerFwdArgs(C.Structure):
     ]
 
 
+class LayerFewArgs(C.Structure):
+    """Mirror of moe_layer_few_args."""
+    _fields_ = [
+        ("struct_size", u32), ("S", i64), ("D", i32), ("E", i32), ("K", i32), ("F", i32), ("Fs", i32),
+        ("score_fn", i32), ("weights", i32),
+        ("x", vp), ("Wr", vp), ("router_bias", vp), ("sel_bias", vp), ("W1", vp), ("W2", vp), ("Ws1", vp),
+        ("Ws2", vp), ("s1", vp), ("s2", vp), ("ss1", vp), ("ss2", vp), ("y", vp), ("topk_idx", vp),
+        ("topk_prob", vp), ("ws", vp), ("ws_bytes", sz),
+    ]
+
+
 SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+WEIGHTS_BF16, WEIGHTS_I8 = 0, 1
+FEW_MAX_TOKENS = 64
 PAYLOAD_BF16, PAYLOAD_MXFP8 = 0, 1
 U8 = torch.uint8
 
@@ -113,6 +126,15 @@ _PROTOS = {
     "moe_mxfp8_dequant": (C.c_int, [vp, vp, i64, i32, vp, vp]),
     "moe_mx_scale_alloc_bytes": (C.c_uint64, [i64, i32]),
     "moe_grouped_gemm_mxfp8": (C.c_int, [vp, vp, vp, i32, i64, i32, i32, vp, i32, vp, vp, vp]),
+    "moe_quant_rows_i8": (C.c_int, [vp, i64, i32, vp, vp, vp]),
+    "moe_quant_weights_i8": (C.c_int, [vp, i32, i32, i32, vp, vp, vp]),
+    "moe_grouped_gemm_i8": (C.c_int, [vp, vp, vp, i32, i64, i32, i32, vp, vp, i32, vp, vp]),
+    "moe_latent_proj_i8_workspace_bytes": (sz, [i64, i32]),
+    "moe_latent_proj_i8": (C.c_int, [vp, vp, vp, i64, i32, i32, vp, vp, sz, vp]),
+    "moe_grouped_ffn_i8_workspace_bytes": (sz, [i32, i64, i32, i32]),
+    "moe_grouped_ffn_i8": (C.c_int, [vp, vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
+    "moe_layer_few_workspace_bytes": (sz, [C.POINTER(LayerFewArgs)]),
+    "moe_layer_few": (C.c_int, [C.POINTER(LayerFewArgs), vp]),
     "moe_shared_expert_bwd": (C.c_int, [vp, vp, vp, vp, vp, vp, i64, i32, i32, vp, i32, vp, vp, vp, sz, vp]),
 }
 
@@ -162,7 +184,15 @@ def _ptr(t: Optional[torch.Tensor], dtype=None, name: str = "tensor"):
     return C.c_void_p(t.data_ptr()) if t.numel() else None
 
 
-BF16, F32, I32 = torch.bfloat16, torch.float32, torch.int32
+def _here(t: Optional[torch.Tensor], dtype=None, name: str = "tensor"):
+    """_ptr of a tensor on the current device, whose stream the call goes to."""
+    p = _ptr(t, dtype, name)
+    if p is not None and t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return p
+
+
+BF16, F32, I32, I8 = torch.bfloat16, torch.float32, torch.int32, torch.int8
 
 
 def moe_abi_version() -> int:
@@ -447,3 +477,74 @@ def moe_grouped_gemm_mxfp8(x_q, x_scale, sched, E, R, Kd, N, W, epilogue, Cout, 
                                          _ptr(sched, None, "sched"), E, R, Kd, N, _ptr(W, BF16, "W"), epilogue,
                                          _ptr(Cout, BF16, "C"), _ptr(u_save, BF16, "u_save"), _stream()),
            "moe_grouped_gemm_mxfp8")
+
+
+def moe_quant_rows_i8(x, R, D, q, scale):
+    _check(load().moe_quant_rows_i8(_here(x, BF16, "x"), R, D, _here(q, I8, "q"), _here(scale, F32, "scale"),
+                                    _stream()), "moe_quant_rows_i8")
+
+
+def moe_quant_weights_i8(W, E, Kd, N, Wq, scale):
+    _check(load().moe_quant_weights_i8(_here(W, BF16, "W"), E, Kd, N, _here(Wq, I8, "Wq"),
+                                       _here(scale, F32, "scale"), _stream()), "moe_quant_weights_i8")
+
+
+def moe_grouped_gemm_i8(Aq, a_scale, sched, E, R, Kd, N, Wq, w_scale, epilogue, Cout):
+    _check(load().moe_grouped_gemm_i8(
+        _here(Aq, I8, "Aq"), _here(a_scale, F32, "a_scale"), _here(sched, None, "sched"), E, R, Kd, N,
+        _here(Wq, I8, "Wq"), _here(w_scale, F32, "w_scale"), epilogue, _here(Cout, BF16, "C"), _stream()),
+        "moe_grouped_gemm_i8")
+
+
+def moe_latent_proj_i8_workspace_bytes(M, Kd) -> int:
+    return load().moe_latent_proj_i8_workspace_bytes(M, Kd)
+
+
+def moe_latent_proj_i8(A, Wq, w_scale, M, Kd, N, Cout, ws):
+    _check(load().moe_latent_proj_i8(
+        _here(A, BF16, "A"), _here(Wq, I8, "Wq"), _here(w_scale, F32, "w_scale"), M, Kd, N, _here(Cout, BF16, "C"),
+        _here(ws, None, "ws"), _wsz(ws), _stream()), "moe_latent_proj_i8")
+
+
+def moe_grouped_ffn_i8_workspace_bytes(E, R, D, F) -> int:
+    return load().moe_grouped_ffn_i8_workspace_bytes(E, R, D, F)
+
+
+def moe_grouped_ffn_i8(x_disp, offsets, E, R, D, F, W1q, s1, W2q, s2, y_disp, ws):
+    _check(load().moe_grouped_ffn_i8(
+        _here(x_disp, BF16, "x_disp"), _here(offsets, I32, "offsets"), E, R, D, F, _here(W1q, I8, "W1q"),
+        _here(s1, F32, "s1"), _here(W2q, I8, "W2q"), _here(s2, F32, "s2"), _here(y_disp, BF16, "y_disp"),
+        _here(ws, None, "ws"), _wsz(ws), _stream()), "moe_grouped_ffn_i8")
+
+
+_FEW_TENSORS = {"x": BF16, "Wr": F32, "router_bias": F32, "sel_bias": F32, "s1": F32, "s2": F32, "ss1": F32,
+                "ss2": F32, "y": BF16, "topk_idx": I32, "topk_prob": F32}
+
+
+def layer_few_args(S, D, E, K, F, Fs=0, score_fn=SCORE_SOFTMAX, weights=WEIGHTS_BF16, ws=None,
+                   **tensors) -> LayerFewArgs:
+    """Fill a moe_layer_few_args from sizes and named tensors (None = NULL)."""
+    a = LayerFewArgs()
+    a.struct_size = C.sizeof(LayerFewArgs)
+    a.S, a.D, a.E, a.K, a.F, a.Fs = S, D, E, K, F, Fs
+    a.score_fn, a.weights = score_fn, weights
+    for name, t in tensors.items():
+        if name in ("W1", "W2", "Ws1", "Ws2"):
+            dtype = I8 if weights == WEIGHTS_I8 else BF16
+        elif name in _FEW_TENSORS:
+            dtype = _FEW_TENSORS[name]
+        else:
+            raise KeyError(name)
+        setattr(a, name, _here(t, dtype, name))
+    if ws is not None:
+        a.ws = _here(ws, None, "ws")
+        a.ws_bytes = _wsz(ws)
+    return a
+
+
+def moe_layer_few_workspace_bytes(args: LayerFewArgs) -> int:
+    return load().moe_layer_few_workspace_bytes(C.byref(args))
+
+
+def moe_layer_few(args: LayerFewArgs):
+    _check(load().moe_layer_few(C.byref(args), _stream()), "moe_layer_few")

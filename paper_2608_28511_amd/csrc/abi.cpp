@@ -35,6 +35,7 @@ int opt(const void* p, size_t align) {
 }
 
 bool dim_ok(int32_t d) { return d >= 8 && d <= kMaxDim && d % 8 == 0; }
+bool dim16_ok(int32_t d) { return d >= 16 && d <= kMaxDim && d % 16 == 0; }   // rows of 8-bit codes
 
 // The grouped GEMM copies operands through buffer descriptors whose range is
 // below 2^31 bytes: one expert's (or the dense) [Kd, N] bf16 weight, and for
@@ -872,6 +873,177 @@ int moe_shared_expert_bwd(const moe_bf16* x, const moe_bf16* u_s, const moe_bf16
     MOE_HIP(moe::launch_dense_wgrad2(h_s, dy, dWs2, Fs, D, x, du, dWs1, D, Fs, S,
                                      (char*)ws + align256((size_t)S * Fs * 2), stream));
     return MOE_OK;
+}
+
+// ---------------------------------------------------------------------------
+// 8-bit weights, and the layer for a few tokens
+// ---------------------------------------------------------------------------
+
+int moe_quant_rows_i8(const moe_bf16* x, int64_t R, int32_t D, int8_t* q, float* scale, hipStream_t stream) {
+    if (R < 0 || R >= kMaxRows || !dim16_ok(D)) return MOE_ERR_SHAPE;
+    MOE_TRY(need(x, (uint64_t)R * D * 2, 16));
+    MOE_TRY(need(q, (uint64_t)R * D, 16));
+    MOE_TRY(need(scale, (uint64_t)R * 4, 4));
+    return hip_status(moe::launch_quant_rows(x, R, D, q, scale, stream));
+}
+
+static int check_i8(int32_t E, int32_t Kd, int32_t N) {
+    if (E < 1 || E > kMaxE || !dim16_ok(Kd) || !dim_ok(N)) return MOE_ERR_SHAPE;
+    if (!weight_ok(Kd, N)) return MOE_ERR_UNSUPPORTED;
+    return MOE_OK;
+}
+
+int moe_quant_weights_i8(const moe_bf16* W, int32_t E, int32_t Kd, int32_t N, int8_t* Wq, float* scale,
+                         hipStream_t stream) {
+    MOE_TRY(check_i8(E, Kd, N));
+    MOE_TRY(need(W, (uint64_t)E * Kd * N * 2, 16));
+    MOE_TRY(need(Wq, (uint64_t)E * Kd * N, 16));
+    MOE_TRY(need(scale, (uint64_t)E * N * 4, 16));
+    return hip_status(moe::launch_quant_weights(W, E, Kd, N, Wq, scale, stream));
+}
+
+int moe_grouped_gemm_i8(const int8_t* Aq, const float* a_scale, const void* sched, int32_t E, int64_t R, int32_t Kd,
+                        int32_t N, const int8_t* Wq, const float* w_scale, int32_t epilogue, moe_bf16* C,
+                        hipStream_t stream) {
+    MOE_TRY(check_i8(E, Kd, N));
+    if (R < 0 || R >= kMaxRows) return MOE_ERR_SHAPE;
+    if (epilogue != 0 && epilogue != 1) return MOE_ERR_UNSUPPORTED;
+    if (sched == nullptr && E != 1) return MOE_ERR_NULL;
+    MOE_TRY(opt(sched, 16));
+    MOE_TRY(need(Aq, (uint64_t)R * Kd, 16));
+    MOE_TRY(need(a_scale, (uint64_t)R * 4, 4));
+    MOE_TRY(need(Wq, (uint64_t)E * Kd * N, 16));
+    MOE_TRY(need(w_scale, (uint64_t)E * N * 4, 16));
+    MOE_TRY(need(C, (uint64_t)R * N * 2, 16));
+    return hip_status(moe::launch_grouped_rows_i8(Aq, a_scale, Wq, w_scale, C, epilogue == 1, sched, E, R, N, Kd,
+                                                  stream));
+}
+
+size_t moe_latent_proj_i8_workspace_bytes(int64_t M, int32_t Kd) {
+    if (M < 0 || M >= kMaxRows || !dim16_ok(Kd)) return 0;
+    return align256((size_t)M * Kd) + align256((size_t)M * 4) + 256;   // 0 says that the sizes are not valid
+}
+
+int moe_latent_proj_i8(const moe_bf16* A, const int8_t* Wq, const float* w_scale, int64_t M, int32_t Kd, int32_t N,
+                       moe_bf16* C, void* ws, size_t ws_bytes, hipStream_t stream) {
+    MOE_TRY(check_i8(1, Kd, N));
+    if (M < 0 || M >= kMaxRows) return MOE_ERR_SHAPE;
+    MOE_TRY(need(A, (uint64_t)M * Kd * 2, 16));
+    MOE_TRY(need(Wq, (uint64_t)Kd * N, 16));
+    MOE_TRY(need(w_scale, (uint64_t)N * 4, 16));
+    MOE_TRY(need(C, (uint64_t)M * N * 2, 16));
+    if (ws == nullptr || ws_bytes < moe_latent_proj_i8_workspace_bytes(M, Kd)) return MOE_ERR_WORKSPACE;
+    MOE_TRY(opt(ws, 256));
+    int8_t* q = (int8_t*)ws;
+    float* scale = (float*)((char*)ws + align256((size_t)M * Kd));
+    MOE_HIP(moe::launch_quant_rows(A, M, Kd, q, scale, stream));
+    return hip_status(moe::launch_grouped_rows_i8(q, scale, Wq, w_scale, C, false, nullptr, 1, M, N, Kd, stream));
+}
+
+namespace {
+
+struct FfnI8Bufs {
+    void* sched; int8_t* xq; float* sx; moe_bf16* h; int8_t* hq; float* sh;
+};
+size_t ffn_i8_layout(int32_t E, int64_t R, int32_t D, int32_t F, char* base, FfnI8Bufs* b) {
+    Carve c{base, 0};
+    b->sched = c.take(moe::gemm_schedule_bytes(E, R));
+    b->sx = (float*)c.take((size_t)R * 4);
+    b->sh = (float*)c.take((size_t)R * 4);
+    // the codes of x are not read after the up projection: those of h take their place
+    b->xq = b->hq = (int8_t*)c.take((size_t)R * (D > F ? D : F));
+    b->h = (moe_bf16*)c.take((size_t)R * F * 2);
+    return c.used;
+}
+
+bool ffn_i8_sizes_ok(int32_t E, int64_t R, int32_t D, int32_t F) {
+    return E >= 1 && E <= kMaxE && R >= 0 && R < kMaxRows && dim16_ok(D) && dim16_ok(F);
+}
+
+}  // namespace
+
+size_t moe_grouped_ffn_i8_workspace_bytes(int32_t E, int64_t R, int32_t D, int32_t F) {
+    if (!ffn_i8_sizes_ok(E, R, D, F)) return 0;
+    FfnI8Bufs b;
+    return ffn_i8_layout(E, R, D, F, nullptr, &b);
+}
+
+int moe_grouped_ffn_i8(const moe_bf16* x_disp, const int32_t* offsets, int32_t E, int64_t R, int32_t D, int32_t F,
+                       const int8_t* W1q, const float* s1, const int8_t* W2q, const float* s2, moe_bf16* y_disp,
+                       void* ws, size_t ws_bytes, hipStream_t stream) {
+    if (!ffn_i8_sizes_ok(E, R, D, F)) return MOE_ERR_SHAPE;
+    if (!weight_ok(D, F)) return MOE_ERR_UNSUPPORTED;
+    MOE_TRY(need(x_disp, (uint64_t)R * D * 2, 16));
+    MOE_TRY(need(offsets, (uint64_t)(E + 1) * 4, 4));
+    MOE_TRY(need(W1q, (uint64_t)E * D * F, 16));
+    MOE_TRY(need(W2q, (uint64_t)E * D * F, 16));
+    MOE_TRY(need(s1, (uint64_t)E * F * 4, 16));
+    MOE_TRY(need(s2, (uint64_t)E * D * 4, 16));
+    MOE_TRY(need(y_disp, (uint64_t)R * D * 2, 16));
+    FfnI8Bufs b;
+    if (ws == nullptr || ws_bytes < ffn_i8_layout(E, R, D, F, nullptr, &b)) return MOE_ERR_WORKSPACE;
+    MOE_TRY(opt(ws, 256));
+    if (R == 0) return MOE_OK;
+    ffn_i8_layout(E, R, D, F, (char*)ws, &b);
+    // the launch that quantises x also builds the tile tables
+    MOE_HIP(moe::launch_quant_rows(x_disp, R, D, b.xq, b.sx, stream, offsets, E, b.sched));
+    MOE_HIP(moe::launch_grouped_rows_i8(b.xq, b.sx, W1q, s1, b.h, true, b.sched, E, R, F, D, stream));
+    MOE_HIP(moe::launch_quant_rows(b.h, R, F, b.hq, b.sh, stream));
+    return hip_status(moe::launch_grouped_rows_i8(b.hq, b.sh, W2q, s2, y_disp, false, b.sched, E, R, D, F, stream));
+}
+
+namespace {
+
+int check_few(const moe_layer_few_args* a) {
+    if (a == nullptr) return MOE_ERR_NULL;
+    if (a->struct_size != sizeof(moe_layer_few_args)) return MOE_ERR_SHAPE;
+    MOE_TRY(check_route_shape(a->S, a->E, a->K));
+    if (a->S > MOE_FEW_MAX_TOKENS) return MOE_ERR_SHAPE;
+    if (a->score_fn != MOE_SCORE_SOFTMAX && a->score_fn != MOE_SCORE_SIGMOID) return MOE_ERR_SHAPE;
+    if (a->weights != MOE_WEIGHTS_BF16 && a->weights != MOE_WEIGHTS_I8) return MOE_ERR_SHAPE;
+    const bool i8 = a->weights == MOE_WEIGHTS_I8;
+    auto dim = [&](int32_t d) { return i8 ? dim16_ok(d) : dim_ok(d); };
+    if (!dim(a->D) || !dim(a->F) || (a->Fs != 0 && !dim(a->Fs))) return MOE_ERR_SHAPE;
+    if (!weight_ok(a->D, a->F) || (a->Fs != 0 && !weight_ok(a->D, a->Fs))) return MOE_ERR_UNSUPPORTED;
+    return MOE_OK;
+}
+
+}  // namespace
+
+size_t moe_layer_few_workspace_bytes(const moe_layer_few_args* a) {
+    if (check_few(a) != MOE_OK || a->S == 0) return 0;
+    return moe::layer_few_ws_bytes(a);
+}
+
+int moe_layer_few(const moe_layer_few_args* a, hipStream_t stream) {
+    MOE_TRY(check_few(a));
+    const bool i8 = a->weights == MOE_WEIGHTS_I8;
+    const uint64_t S = a->S, D = a->D, E = a->E, F = a->F, Fs = a->Fs, wb = i8 ? 1 : 2;
+    if (a->score_fn == MOE_SCORE_SOFTMAX && a->sel_bias != nullptr) return MOE_ERR_SHAPE;
+    if (Fs == 0 && (a->Ws1 != nullptr || a->Ws2 != nullptr || a->ss1 != nullptr || a->ss2 != nullptr))
+        return MOE_ERR_SHAPE;
+    if (!i8 && (a->s1 != nullptr || a->s2 != nullptr || a->ss1 != nullptr || a->ss2 != nullptr)) return MOE_ERR_SHAPE;
+    MOE_TRY(need(a->x, S * D * 2, 16));
+    MOE_TRY(need(a->Wr, D * E * 4, 4));
+    MOE_TRY(opt(a->router_bias, 4));
+    MOE_TRY(opt(a->sel_bias, 4));
+    MOE_TRY(need(a->W1, E * D * F * wb, 16));
+    MOE_TRY(need(a->W2, E * D * F * wb, 16));
+    MOE_TRY(need(a->Ws1, D * Fs * wb, 16));
+    MOE_TRY(need(a->Ws2, D * Fs * wb, 16));
+    if (i8) {
+        MOE_TRY(need(a->s1, E * F * 4, 16));
+        MOE_TRY(need(a->s2, E * D * 4, 16));
+        MOE_TRY(need(a->ss1, Fs * 4, 16));
+        MOE_TRY(need(a->ss2, Fs ? D * 4 : 0, 16));
+    }
+    MOE_TRY(need(a->y, S * D * 2, 16));
+    MOE_TRY(opt(a->topk_idx, 4));
+    MOE_TRY(opt(a->topk_prob, 4));
+    if (S == 0) return MOE_OK;
+    if (a->ws == nullptr || a->ws_bytes < moe::layer_few_ws_bytes(a)) return MOE_ERR_WORKSPACE;
+    MOE_TRY(opt(a->ws, 256));
+    return hip_status(moe::launch_layer_few(a, stream));
 }
 
 }  // extern "C"

@@ -205,6 +205,8 @@ struct GemmArgs {
     uint32_t a_mul;           // v / a_div = v * a_mul >> a_shift for 0 <= v < 2^31
     int a_shift;
     int64_t a_src_rows;       // rows of the gathered A
+    const float* row_scale;   // 8-bit products: scale of each row of A
+    const float* col_scale;   // ... and of each expert's output columns [E, N]
     const uint8_t* A_scale;   // MX-FP8 A: E8M0 scales [R, Kd / 32]
     uint32_t scale_bytes;     // R * Kd / 32 rounded up to a multiple of 4
     int64_t lda, ldb, ldc;
@@ -240,7 +242,7 @@ __device__ __forceinline__ void wait_stage(int cur, int total) {
 // and accumulate.  `next` says whether there is a stage to copy; nrem is the
 // contraction length left from its start.
 // AMX: sb is the lane's scale byte of the stage's first block in slot 0.
-template <class T, bool A_K, bool B_K, bool KTAIL, int S, class DA, class DB, int NA, int NB>
+template <class T, bool A_K, bool B_K, bool KTAIL, int S, bool I8 = false, class DA, class DB, int NA, int NB>
 __device__ __forceinline__ void mma_stage(f32x4 (&acc)[T::MI][4], const uint32_t (&abase)[NA],
                                           const uint32_t (&bbase)[2][NB], DA& da, DB& db, bool next,
                                           int64_t nrem, uint32_t ldsA, uint32_t ldsB, int wave,
@@ -288,7 +290,7 @@ __device__ __forceinline__ void mma_stage(f32x4 (&acc)[T::MI][4], const uint32_t
         for (int i = 0; i < T::MI; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bfg[j], af[i], acc[i][j], 0, 0, 0);
+                acc[i][j] = mfma16<I8>(bfg[j], af[i], acc[i][j]);
     }
 }
 
@@ -625,8 +627,29 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const void* base, in
 constexpr uint32_t kDropOffset = 0x80000000u;  // beyond any descriptor's range
 constexpr int kNonTemporal = 2;                // cache policy of a buffer store
 
+// The scales of a wave tile of an 8-bit product at the accumulators' positions:
+// lane's rows 16 i + lane % 16 and columns 16 j + 4 (lane / 16) .. + 3 (zero outside).
+template <int MI>
+struct I8Scales {
+    float row[MI];
+    f32x4 col[4];
+    __device__ __forceinline__ void load(const GemmArgs& p, int e, int rbase, int nrows, int cbase, int lane) {
+        const __amdgpu_buffer_rsrc_t rr = __builtin_amdgcn_make_buffer_rsrc(
+            (void*)(p.row_scale + rbase), 0, nrows > 0 ? nrows * 4 : 0, 0x00020000);
+        const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(
+            (void*)(p.col_scale + (int64_t)e * p.N), 0, p.N * 4, 0x00020000);
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+            row[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rr, (uint32_t)(i * 16 + (lane & 15)) * 4, 0, 0));
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            col[j] = __builtin_bit_cast(
+                f32x4, __builtin_amdgcn_raw_buffer_load_b128(rc, (uint32_t)(cbase + j * 16 + 4 * (lane >> 4)) * 4, 0, 0));
+    }
+};
+
 // Staged epilogue of one 64 x 64 wave tile (EPI_BF16 / EPI_RELU2 /
-// EPI_DRELU2): per 16-row block, the accumulators go to the wave's LDS slice
+// EPI_DRELU2, and the scaled 8-bit products): per 16-row block, the accumulators go to the wave's LDS slice
 // as bf16 (chunk c of row r at c ^ (r & 7)), come back as 16-byte row pieces
 // and leave as two buffer_store_dwordx4 of 8 rows x 128 bytes each.  OUT:
 // 0 = the product (squared-ReLU applied for EPI_RELU2; times 2 max(u, 0),
@@ -635,7 +658,8 @@ constexpr int kNonTemporal = 2;                // cache policy of a buffer store
 template <int EPI, int OUT, int MI>
 __device__ __forceinline__ void staged_store(const f32x4 (&acc)[MI][4], void* C, int64_t ldc, int N,
                                              int64_t rbase, int64_t nrows, int64_t cbase,
-                                             uint32_t ep, int lane, const u32x2 (*uu)[4] = nullptr) {
+                                             uint32_t ep, int lane, const u32x2 (*uu)[4] = nullptr,
+                                             const I8Scales<MI>* sc = nullptr) {
     const __amdgpu_buffer_rsrc_t rs = rows_rsrc(C, rbase, nrows, ldc);
     const int r = lane & 15;
     const uint32_t wr = ep + (uint32_t)(r * 128 + (lane >> 4 & 1) * 8);
@@ -648,7 +672,14 @@ __device__ __forceinline__ void staged_store(const f32x4 (&acc)[MI][4], void* C,
         for (int j = 0; j < 4; ++j) {
             const f32x4 a = acc[i][j];
             float v0 = a[0], v1 = a[1], v2 = a[2], v3 = a[3];
-            if constexpr (EPI == EPI_RELU2 && OUT == 0) {
+            if constexpr (epi_i8(EPI)) {
+                const float r = sc->row[i];
+                v0 = (float)__float_as_int(v0) * r * sc->col[j][0];
+                v1 = (float)__float_as_int(v1) * r * sc->col[j][1];
+                v2 = (float)__float_as_int(v2) * r * sc->col[j][2];
+                v3 = (float)__float_as_int(v3) * r * sc->col[j][3];
+            }
+            if constexpr ((EPI == EPI_RELU2 || EPI == EPI_I8_RELU2) && OUT == 0) {
                 v0 = relu_f32(v0); v1 = relu_f32(v1); v2 = relu_f32(v2); v3 = relu_f32(v3);
                 v0 *= v0; v1 *= v1; v2 *= v2; v3 *= v3;
             }
@@ -832,8 +863,8 @@ __device__ __forceinline__ void rows_body(const GemmArgs& p, char* smem, const i
         if (next && kd == 0) dma_tile(jd);
         uint32_t sb = 0;
         if constexpr (T::kAmx) sb = sbase + (((uint32_t)(cur.row0 * nb + kc * T::kKK) + rnb) & 3u);
-        mma_stage<T, true, B_K, KTAIL, S>(acc, abase, bbase, da, db, next, p.Kd - kd * KD, ldsA, ldsB, wave,
-                                          sb);
+        mma_stage<T, true, B_K, KTAIL, S, epi_i8(EPI)>(acc, abase, bbase, da, db, next, p.Kd - kd * KD, ldsA, ldsB,
+                                                       wave, sb);
         if (++kd == nk) { kd = 0; ++jd; }
         if (kc == nk - 1) {
             const int rbase = cur.row0 + wm * T::kWaveRows;
@@ -843,6 +874,10 @@ __device__ __forceinline__ void rows_body(const GemmArgs& p, char* smem, const i
                 staged_store<EPI, 0, MI>(acc, p.C, p.ldc, p.N, rbase, nrows, cbase, ep, lane, uu);
             } else if constexpr (EPI == EPI_F32) {
                 f32_store(acc, (float*)p.C, p.ldc, p.N, rbase, nrows, cbase, p.accumulate != 0, lane);
+            } else if constexpr (epi_i8(EPI)) {
+                I8Scales<MI> sc;
+                sc.load(p, cur.e, rbase, nrows, cbase, lane);
+                staged_store<EPI, 0, MI>(acc, p.C, p.ldc, p.N, rbase, nrows, cbase, ep, lane, nullptr, &sc);
             } else {
                 staged_store<EPI, 0, MI>(acc, p.C, p.ldc, p.N, rbase, nrows, cbase, ep, lane);
                 if constexpr (EPI == EPI_RELU2)
@@ -959,7 +994,8 @@ __device__ __forceinline__ void rows_list_phased(const GemmArgs& p, char* smem, 
         return u;
     };
 
-    Phased<true, B_K, KTAIL> ph;
+    using PH = Phased<true, B_K, KTAIL, epi_i8(EPI)>;
+    PH ph;
     ph.wave = wave;
     ph.bases(lds0, wm, wn, lane_);
     ph.nkd = nk;
@@ -978,7 +1014,6 @@ __device__ __forceinline__ void rows_list_phased(const GemmArgs& p, char* smem, 
     // nxt: the tile after the one being sent; its operands' descriptors and, with
     // gathered rows, its chunks are prepared where both groups are in step.
     // ahead: the tile after that one, whose perm entries are on their way.
-    using PH = Phased<true, B_K, KTAIL>;
     struct Next {
         i32x4 a, b;
         int cols;
@@ -1061,9 +1096,14 @@ __device__ __forceinline__ void rows_list_phased(const GemmArgs& p, char* smem, 
         const int lane = fresh(lane_);
         // tile jc + 2 (jc + 1 is being sent); its perm entries landed during this tile's second k tile
         if (jc + 2 < n_mine) prepare();
+        I8Scales<4> sc0, sc1;
+        if constexpr (epi_i8(EPI)) {
+            sc0.load(p, cur.e, r0, cur.row_hi - r0, cbase, lane);
+            sc1.load(p, cur.e, r0 + 128, cur.row_hi - (r0 + 128), cbase, lane);
+        }
         wait_vmcnt<0>();   // the next k tile is a FRESH one
         if (jc + 3 < n_mine) look_ahead(jc + 3);
-        auto leave = [&](const f32x4 (&acc)[4][4], int rbase) {
+        auto leave = [&](const f32x4 (&acc)[4][4], int rbase, [[maybe_unused]] const I8Scales<4>& sc) {
             const int nrows = cur.row_hi - rbase;
             if constexpr (EPI == EPI_DRELU2) {
                 u32x2 uu[4][4];
@@ -1071,6 +1111,8 @@ __device__ __forceinline__ void rows_list_phased(const GemmArgs& p, char* smem, 
                 staged_store<EPI, 0, 4>(acc, p.C, p.ldc, p.N, rbase, nrows, cbase, ep, lane, uu);
             } else if constexpr (EPI == EPI_F32) {
                 f32_store(acc, (float*)p.C, p.ldc, p.N, rbase, nrows, cbase, p.accumulate != 0, lane);
+            } else if constexpr (epi_i8(EPI)) {
+                staged_store<EPI, 0, 4>(acc, p.C, p.ldc, p.N, rbase, nrows, cbase, ep, lane, nullptr, &sc);
             } else {
                 staged_store<EPI, 0, 4>(acc, p.C, p.ldc, p.N, rbase, nrows, cbase, ep, lane);
                 if constexpr (EPI == EPI_RELU2)
@@ -1078,8 +1120,8 @@ __device__ __forceinline__ void rows_list_phased(const GemmArgs& p, char* smem, 
                         staged_store<EPI, 1, 4>(acc, p.aux_out, p.ldc, p.N, rbase, nrows, cbase, ep, lane);
             }
         };
-        if (on0) leave(acc0, r0);
-        if (on1) leave(acc1, r0 + 128);
+        if (on0) leave(acc0, r0, sc0);
+        if (on1) leave(acc1, r0 + 128, sc1);
         if (jc + 1 < n_mine) cur = tile_at(jc + 1);
     }
     wait_vmcnt<0>();   // no copy into LDS outlives the workgroup
@@ -1611,6 +1653,8 @@ static hipError_t launch_rows_epi(const GemmArgs& a, bool b_kmajor, int epi, hip
         if (epi == EPI_BF16) return launch_rows<true, EPI_BF16>(a, st);
         if (epi == EPI_DRELU2) return launch_rows<true, EPI_DRELU2>(a, st);
         if (epi == EPI_F32) return launch_rows<true, EPI_F32>(a, st);
+        if (epi == EPI_I8_BF16) return launch_rows<true, EPI_I8_BF16>(a, st);
+        if (epi == EPI_I8_RELU2) return launch_rows<true, EPI_I8_RELU2>(a, st);
     }
     return hipErrorInvalidValue;
 }
@@ -1699,6 +1743,21 @@ hipError_t launch_grouped_rows_mx(const uint8_t* Aq, const uint8_t* A_scale, con
     return hipErrorInvalidValue;
 }
 
+
+hipError_t launch_grouped_rows_i8(const int8_t* A, const float* a_scale, const int8_t* B, const float* b_scale,
+                                  void* C, bool relu2, const void* sched, int E, int64_t R, int N, int Kd,
+                                  hipStream_t st) {
+    if (R == 0) return hipSuccess;
+    if (Kd <= 0 || Kd % 16 != 0 || N % 8 != 0) return hipErrorInvalidValue;
+    // two codes to a 16-bit element: the bf16 tiles of half the contraction
+    GemmArgs a{};
+    a.A = (const uint16_t*)A;
+    a.lda = Kd / 2;
+    a.row_scale = a_scale;
+    a.col_scale = b_scale;
+    rows_args(a, (const moe_bf16*)B, Kd / 2, (int64_t)N * (Kd / 2), C, N, nullptr, sched, E, R, N, Kd / 2);
+    return launch_rows_epi(a, true, relu2 ? EPI_I8_RELU2 : EPI_I8_BF16, st);
+}
 
 constexpr int kPhasedGradPct = 152;   // cost of a round of phased items, of one of 128-row items
 

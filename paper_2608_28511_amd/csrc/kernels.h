@@ -12,7 +12,8 @@ namespace moe {
 // Experts of a layer: every kernel's per-expert tables in LDS hold this many.
 constexpr int kMaxExperts = 1024;
 
-enum { EPI_BF16 = 0, EPI_RELU2 = 1, EPI_DRELU2 = 2, EPI_F32 = 3 };
+enum { EPI_BF16 = 0, EPI_RELU2 = 1, EPI_DRELU2 = 2, EPI_F32 = 3, EPI_I8_BF16 = 4, EPI_I8_RELU2 = 5 };
+constexpr bool epi_i8(int epi) { return epi == EPI_I8_BF16 || epi == EPI_I8_RELU2; }   // scaled products of 8-bit integers
 
 // Compute units of the current device (read once per device).
 int cu_count();
@@ -109,6 +110,22 @@ hipError_t launch_grouped_rows_gather(const moe_bf16* X, int64_t ldx, int64_t x_
 hipError_t launch_grouped_rows_mx(const uint8_t* Aq, const uint8_t* A_scale, const moe_bf16* B, int64_t ldb,
                                   int64_t b_stride, void* C, int64_t ldc, int epi, moe_bf16* aux_out,
                                   const void* sched, int E, int64_t R, int N, int Kd, hipStream_t st);
+// ROWS mode in 8-bit integers: C[r, n] = bf16(a_scale[r] * b_scale[e, n] * sum_k A[r, k] B_e[n, k]), with relu2
+// bf16(max(., 0)^2).  A [R, Kd], B [E, N, Kd] int8 (16-byte aligned, Kd a multiple of 16), exact 32-bit sums; sched
+// as in launch_grouped_rows.
+hipError_t launch_grouped_rows_i8(const int8_t* A, const float* a_scale, const int8_t* B, const float* b_scale,
+                                  void* C, bool relu2, const void* sched, int E, int64_t R, int N, int Kd,
+                                  hipStream_t st);
+// 8-bit rows: scale[r] = max|x[r, :]| / 127 and the codes of x[r, :] (quant.hip).  With sched (and offsets
+// [E+1] of the same rows), the launch also builds the grouped GEMM's tile tables.
+hipError_t launch_quant_rows(const moe_bf16* x, int64_t R, int D, int8_t* q, float* scale, hipStream_t st,
+                             const int32_t* sched_offsets = nullptr, int E = 0, void* sched = nullptr);
+// The same per output channel: W [E, Kd, N] bf16 -> Wq [E, N, Kd] int8, scale [E, N].
+hipError_t launch_quant_weights(const moe_bf16* W, int E, int Kd, int N, int8_t* Wq, float* scale, hipStream_t st);
+// The whole layer for at most kFewMaxTokens tokens (few.hip); arguments validated, workspace bound.
+constexpr int kFewMaxTokens = MOE_FEW_MAX_TOKENS;
+size_t layer_few_ws_bytes(const moe_layer_few_args* a);
+hipError_t launch_layer_few(const moe_layer_few_args* a, hipStream_t st);
 // KGRP mode: C_e[m, n] = sum over expert e's rows r of A[r, m] * B[r, n]  (fp32 out).
 // Dense weight gradients C_q [M_q, N_q] = A_q^T B_q over R rows (fp32 out, row-major and contiguous operands),
 // two at once or (M1 = N1 = 0) one; ws of dense_wgrad_ws_bytes holds the partial tiles.

@@ -142,9 +142,11 @@ struct PieceDma {
 };
 
 // The k-tile stream of one workgroup.  next_tile(da, db) starts the copies of
-// the output tile that follows (or stops them past the last one).
-template <bool A_ROW, bool B_ROW, bool KTAIL>
+// the output tile that follows (or stops them past the last one).  I8: 8-bit
+// operands, two to a 16-bit element.
+template <bool A_ROW, bool B_ROW, bool KTAIL, bool I8 = false>
 struct Phased {
+    static_assert(!I8 || (A_ROW && B_ROW), "8-bit fragments come from the row layout");
     using DA = PieceDma<A_ROW, false>;
     using DB = PieceDma<B_ROW, !B_ROW>;
     DA da;
@@ -211,7 +213,7 @@ struct Phased {
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], acc[i][j], 0, 0, 0);
+                    acc[i][j] = mfma16<I8>(b[j], a[i], acc[i][j]);
             __builtin_amdgcn_s_setprio(0);
         }
         __builtin_amdgcn_sched_barrier(0);

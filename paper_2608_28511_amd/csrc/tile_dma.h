@@ -233,6 +233,21 @@ __device__ __forceinline__ uint32_t col_base(int col0, int lane) {
     return (uint32_t)((k * kCPR + (c ^ cswz(k))) * 16 + (q & 1) * 8);
 }
 
+// One matrix product step of a pair of 16-byte fragments (16 rows or columns x
+// 16 bytes of the contraction per lane group): 32 deep in bf16, or 64 deep in 8-bit
+// integers, whose 32-bit integer sums travel in the same accumulator registers.
+// Both take the same time, so 8-bit operands of half the bytes run the same
+// tiles, with the same copies and fragment reads, at twice the rate.
+template <bool I8>
+__device__ __forceinline__ f32x4 mfma16(bf16x8 b, bf16x8 a, f32x4 c) {
+    if constexpr (I8)
+        return __builtin_bit_cast(
+            f32x4, __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, b), __builtin_bit_cast(i32x4, a),
+                                                         __builtin_bit_cast(i32x4, c), 0, 0, 0));
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, a, c, 0, 0, 0);
+}
+
 typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
 
 __device__ __forceinline__ bf16x8 lds_b128(uint32_t addr) { return *(const lds_bf16x8*)(uintptr_t)addr; }

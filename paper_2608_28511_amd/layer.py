@@ -9,7 +9,7 @@ import torch
 
 from . import _lib as L
 
-BF16, F32, I32 = torch.bfloat16, torch.float32, torch.int32
+BF16, F32, I32, I8 = torch.bfloat16, torch.float32, torch.int32, torch.int8
 
 
 def _empty(shape, dtype, device):
@@ -339,3 +339,120 @@ class LayerFwd:
                              Ws1=Ws1, Ws2=Ws2, **self._modes(), **self.out)
         L.moe_layer_fwd(a)
         return self.out
+
+
+def quant_rows_i8(x: torch.Tensor):
+    """8-bit rows of activations: (q int8 like x, scale fp32 [R])."""
+    R, D = x.shape
+    q = _empty((R, D), I8, x.device)
+    scale = _empty((R,), F32, x.device)
+    L.moe_quant_rows_i8(x, R, D, q, scale)
+    return q, scale
+
+
+def quant_weights_i8(W: torch.Tensor):
+    """8-bit output channels of W [E, Kd, N] or [Kd, N]: (Wq int8 [E, N, Kd] or
+    [N, Kd], scale fp32 [E, N] or [N]), as the 8-bit products read them."""
+    if W.dim() == 2:
+        Wq, scale = quant_weights_i8(W[None])
+        return Wq[0], scale[0]
+    E, Kd, N = W.shape
+    Wq = _empty((E, N, Kd), I8, W.device)
+    scale = _empty((E, N), F32, W.device)
+    L.moe_quant_weights_i8(W, E, Kd, N, Wq, scale)
+    return Wq, scale
+
+
+def _sizes(ok: bool, what: str):
+    if not ok:
+        raise ValueError(f"sizes of {what} do not fit together")
+
+
+def grouped_gemm_i8(Aq, a_scale, sched, Wq, w_scale, epilogue: int, out: Optional[torch.Tensor] = None):
+    """One product of 8-bit rows with 8-bit expert weights [E, N, Kd] (sched None: one dense weight, E = 1)."""
+    R, Kd = Aq.shape
+    E, N, _ = Wq.shape
+    _sizes(a_scale.shape == (R,) and Wq.shape[2] == Kd and w_scale.shape == (E, N), "Aq, Wq and their scales")
+    C = out if out is not None else _empty((R, N), BF16, Aq.device)
+    _sizes(C.shape == (R, N), "out")
+    L.moe_grouped_gemm_i8(Aq, a_scale, sched, E, R, Kd, N, Wq, w_scale, epilogue, C)
+    return C
+
+
+def latent_proj_i8(A: torch.Tensor, Wq: torch.Tensor, w_scale: torch.Tensor):
+    """latent_proj with an 8-bit weight [N, Kd]; the rows of A are quantised in the call."""
+    M, Kd = A.shape
+    N = Wq.shape[0]
+    _sizes(Wq.shape == (N, Kd) and w_scale.shape == (N,), "A, Wq and w_scale")
+    C = _empty((M, N), BF16, A.device)
+    ws = _ws(L.moe_latent_proj_i8_workspace_bytes(M, Kd), A.device)
+    L.moe_latent_proj_i8(A, Wq, w_scale, M, Kd, N, C, ws)
+    return C
+
+
+def grouped_ffn_i8(x_disp, offsets, W1q, s1, W2q, s2):
+    """grouped_ffn with 8-bit weights W1q [E, F, D], W2q [E, D, F] and their scales; returns y_disp."""
+    R, D = x_disp.shape
+    E, F, _ = W1q.shape
+    _sizes(W1q.shape == (E, F, D) and W2q.shape == (E, D, F) and s1.shape == (E, F) and s2.shape == (E, D)
+           and offsets.shape == (E + 1,), "x_disp, offsets, weights and scales")
+    dev = x_disp.device
+    y_disp = _empty((R, D), BF16, dev)
+    ws = _ws(L.moe_grouped_ffn_i8_workspace_bytes(E, R, D, F), dev)
+    L.moe_grouped_ffn_i8(x_disp, offsets, E, R, D, F, W1q, s1, W2q, s2, y_disp, ws)
+    return y_disp
+
+
+class LayerFew:
+    """One layer's weights, with buffers for moe_layer_few calls of up to S tokens.
+
+    Weights are bf16 (W1 [E, D, F], W2 [E, F, D], as LayerFwd takes them) or, with the
+    channel scales s1 and s2 given, int8 as quant_weights_i8 returns them; the shared
+    expert's (Ws1, Ws2, with ss1 and ss2) likewise.  A call takes x [n, D] of any
+    n <= S tokens and returns y [n, D], topk_idx and topk_prob [n, K], which the next call
+    overwrites.  Calls of one object share its workspace: on several streams, or
+    replayed from several graphs, they must be ordered; objects are independent.
+    """
+
+    def __init__(self, S, Wr, W1, W2, K, bias=None, sel_bias=None, score="softmax", s1=None, s2=None, Ws1=None,
+                 Ws2=None, ss1=None, ss2=None):
+        i8 = s1 is not None
+        E, D, F = W1.shape if not i8 else (W1.shape[0], W1.shape[2], W1.shape[1])
+        Fs = 0 if Ws1 is None else Ws1.shape[0 if i8 else 1]
+        io = (lambda a, b: (b, a)) if i8 else (lambda a, b: (a, b))
+        want = {"Wr": (D, E), "bias": (E,), "sel_bias": (E,), "W2": (E,) + io(F, D), "s1": (E, F), "s2": (E, D),
+                "Ws1": io(D, Fs), "Ws2": io(Fs, D), "ss1": (Fs,), "ss2": (D,)}
+        given = dict(Wr=Wr, bias=bias, sel_bias=sel_bias, W2=W2, s1=s1, s2=s2, Ws1=Ws1, Ws2=Ws2, ss1=ss1, ss2=ss2)
+        for name, t in given.items():
+            _sizes(t is None or tuple(t.shape) == tuple(want[name]), name)
+        if (s2 is None) == i8 or any((t is None) != (Fs == 0) for t in ((Ws1, Ws2, ss1, ss2) if i8 else (Ws1, Ws2))):
+            raise ValueError("weights and scales must be given together")
+        if sel_bias is not None and score != "sigmoid":
+            raise ValueError("sel_bias goes with sigmoid scores")
+        dev = W1.device
+        self.S, self.D, self.K = S, D, K
+        self.out = dict(y=_empty((S, D), BF16, dev), topk_idx=_empty((S, K), I32, dev),
+                        topk_prob=_empty((S, K), F32, dev))
+        self.weights = dict(given, W1=W1)   # held as long as the pointers are used
+        self._args = L.layer_few_args(
+            S, D, E, K, F, Fs, {"softmax": L.SCORE_SOFTMAX, "sigmoid": L.SCORE_SIGMOID}[score],
+            L.WEIGHTS_I8 if i8 else L.WEIGHTS_BF16, Wr=Wr, router_bias=bias, sel_bias=sel_bias, W1=W1, W2=W2, Ws1=Ws1,
+            Ws2=Ws2, s1=s1, s2=s2, ss1=ss1, ss2=ss2, **self.out)
+        # a smaller call may share its contractions among more workgroups, whose sums take more room
+        sizes = []
+        for n in range(1, S + 1):
+            self._args.S = n
+            sizes.append(L.moe_layer_few_workspace_bytes(self._args))
+        if S > 0 and min(sizes) == 0:
+            raise ValueError("invalid layer shape")
+        self.ws = _ws(max(sizes, default=1), dev)
+        self._args.ws, self._args.ws_bytes = self.ws.data_ptr(), self.ws.numel()
+
+    def __call__(self, x: torch.Tensor) -> Dict[str, torch.Tensor]:
+        n, D = x.shape
+        _sizes(D == self.D and n <= self.S, "x")
+        a = self._args
+        a.S = n
+        a.x = L._here(x, BF16, "x")
+        L.moe_layer_few(a)
+        return self.out if n == self.S else {k: v[:n] for k, v in self.out.items()}

@@ -1,0 +1,288 @@
+"""moe_layer_few against the layer's definition in 64 bits.
+
+Logits are sums of D exact products in fp32: chains of 16, two joins, ceil(D / 64)
+partial sums and the bias, so each is within (19 + ceil(D / 64)) 2^-24 of the sum of its
+terms' magnitudes; tau is a token's largest such error.  Picks may differ from 64 bits by
+2 tau, weights by 2 tau + 2^-20 of their value (the exponential and the division).
+bf16 weights: y's bound is elementwise.  Each expert's term carries the errors of
+serving_oracle.ffn_bound and its weight's; K + 1 terms are summed in fp32 and rounded once
+to bf16.
+8-bit weights: the codes and integer sums are those of moe_grouped_ffn_i8, whose y_disp is
+rounded to bf16 once more.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import moe_oracle as O
+from oracle import serving_oracle as V
+from paper_2608_28511_amd import _lib as L
+from paper_2608_28511_amd import layer
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16 = torch.bfloat16
+
+
+def np64(t):
+    return t.detach().cpu().double().numpy()
+
+
+class Model:
+    """Weights of one layer; the experts' bf16 values are kept beside their 8-bit form."""
+
+    def __init__(self, D, E, K, F, Fs=0, score="softmax", weights="bf16", seed=0, bias_std=0.3):
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        n = lambda shape, std: torch.randn(shape, generator=g, device=DEV) * std  # noqa: E731
+        self.D, self.E, self.K, self.F, self.Fs, self.score, self.weights = D, E, K, F, Fs, score, weights
+        self.Wr = n((D, E), D ** -0.5)
+        self.bias = n((E,), bias_std)
+        self.sel = n((E,), 0.05) if score == "sigmoid" else None
+        self.W1, self.W2 = n((E, D, F), D ** -0.5).to(BF16), n((E, F, D), F ** -0.5).to(BF16)
+        self.kw = dict(bias=self.bias, sel_bias=self.sel, score=score)
+        if Fs:
+            self.Ws1, self.Ws2 = n((D, Fs), D ** -0.5).to(BF16), n((Fs, D), Fs ** -0.5).to(BF16)
+        if weights == "i8":
+            self.w1, self.s1 = layer.quant_weights_i8(self.W1)
+            self.w2, self.s2 = layer.quant_weights_i8(self.W2)
+            self.kw.update(s1=self.s1, s2=self.s2)
+            if Fs:
+                self.ws1, self.ss1 = layer.quant_weights_i8(self.Ws1)
+                self.ws2, self.ss2 = layer.quant_weights_i8(self.Ws2)
+                self.kw.update(Ws1=self.ws1, Ws2=self.ws2, ss1=self.ss1, ss2=self.ss2)
+        else:
+            self.w1, self.w2 = self.W1, self.W2
+            if Fs:
+                self.kw.update(Ws1=self.Ws1, Ws2=self.Ws2)
+
+    def layer(self, S):
+        return layer.LayerFew(S, self.Wr, self.w1, self.w2, self.K, **self.kw)
+
+    def tokens(self, S, seed=1):
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        return torch.randn((S, self.D), generator=g, device=DEV).to(BF16)
+
+    def picks(self, x):
+        """(selection scores, weights of given picks) in 64 bits."""
+        logits = np64(x) @ np64(self.Wr) + np64(self.bias)
+        if self.score == "sigmoid":
+            act = 1 / (1 + np.exp(-logits))
+            return act + np64(self.sel), act
+        return logits, np.exp(logits - logits.max(1, keepdims=True))
+
+
+def check_picks(m, x, idx, prob):
+    """The weights of the picks in 64 bits, and their relative error's bound per token."""
+    sel, act = m.picks(x)
+    S, K = idx.shape
+    mag = np.abs(np64(x)) @ np.abs(np64(m.Wr)) + np.where(np.isfinite(np64(m.bias)), np.abs(np64(m.bias)), 0)
+    tau = (19 + -(-m.D // 64)) * 2.0 ** -24 * mag.max(1)
+    assert ((idx >= 0) & (idx < m.E)).all()
+    got = np.take_along_axis(sel, idx, 1)
+    for t in range(S):
+        assert len(set(idx[t])) == K
+        assert np.all(got[t][:-1] >= got[t][1:] - 2 * tau[t] - 2.0 ** -22)
+        rest = np.delete(sel[t], idx[t])
+        assert rest.size == 0 or got[t].min() >= rest.max() - 2 * tau[t] - 2.0 ** -22
+    w = np.take_along_axis(act, idx, 1)
+    ref = w / w.sum(1, keepdims=True)
+    eps = (2 * tau + 2.0 ** -20)[:, None]
+    assert np.all(np.abs(prob - ref) <= eps * ref)
+    return ref, eps
+
+
+def check_bf16(m, x, out):
+    idx, y = out["topk_idx"].cpu().numpy().astype(int), np64(out["y"])
+    p, eps = check_picks(m, x, idx, np64(out["topk_prob"]))
+    xs = np64(x)
+    ref, tol = np.zeros_like(xs), np.zeros_like(xs)
+    for e in sorted(set(idx.ravel())):
+        t, k = np.nonzero(idx == e)
+        v, b = V.ffn_bound(xs[t], np64(m.W1[e]), np64(m.W2[e]))
+        w = p[t, k][:, None]
+        ref[t] += w * v
+        tol[t] += w * (b + (eps[t] + (m.K + 1) * 2.0 ** -24) * (np.abs(v) + b))
+    if m.Fs:
+        v, b = V.ffn_bound(xs, np64(m.Ws1), np64(m.Ws2))
+        ref += v
+        tol += b + (m.K + 1) * 2.0 ** -24 * (np.abs(v) + b)
+    assert np.all(np.abs(y - ref) <= tol + 2.0 ** -8 * (np.abs(ref) + tol))
+
+
+def check_i8(m, x, out):
+    """Against moe_grouped_ffn_i8 on the same picks."""
+    idx = out["topk_idx"].long()
+    S, K = idx.shape
+    p, eps = (torch.tensor(a, device=DEV) for a in check_picks(m, x, idx.cpu().numpy(), np64(out["topk_prob"])))
+    order = torch.sort(idx.reshape(-1), stable=True).indices
+    off = torch.zeros(m.E + 1, dtype=torch.int32, device=DEV)
+    off[1:] = torch.bincount(idx.reshape(-1), minlength=m.E).cumsum(0)
+    yd = layer.grouped_ffn_i8(x[order // K].contiguous(), off, m.w1, m.s1, m.w2, m.s2).double()
+    rows = torch.empty_like(yd)
+    rows[order] = yd
+    terms = rows.view(S, K, -1) * p[..., None]
+    ref, mag = terms.sum(1), terms.abs().sum(1)
+    if m.Fs:
+        off = torch.tensor([0, S], dtype=torch.int32, device=DEV)
+        s = layer.grouped_ffn_i8(x, off, m.ws1[None], m.ss1[None], m.ws2[None], m.ss2[None]).double()
+        ref, mag = ref + s, mag + s.abs()
+    tol = mag * (2.0 ** -8 + eps + (K + 4) * 2.0 ** -24) + ref.abs() * 2.0 ** -8
+    assert bool(((out["y"].double() - ref).abs() <= tol * (1 + 2.0 ** -7)).all())
+
+
+SHAPES = [   # S, D, E, K, F, Fs, score
+    (1, 16, 1, 1, 16, 0, "softmax"), (2, 64, 8, 8, 48, 0, "softmax"), (3, 272, 65, 5, 176, 0, "sigmoid"),
+    (1, 2048, 64, 6, 1024, 0, "softmax"), (5, 672, 512, 22, 336, 0, "softmax"), (7, 336, 24, 3, 528, 400, "sigmoid"),
+    (17, 1040, 16, 2, 272, 0, "softmax"), (33, 128, 4, 2, 1040, 64, "softmax"), (64, 256, 3, 2, 512, 256, "sigmoid"),
+    (64, 512, 1, 1, 80, 0, "softmax"), (64, 144, 1024, 32, 32, 0, "softmax"), (49, 64, 130, 32, 96, 16, "sigmoid")]
+
+
+@pytest.mark.parametrize("weights", ["bf16", "i8"])
+@pytest.mark.parametrize("S, D, E, K, F, Fs, score", SHAPES)
+def test_layer_few(S, D, E, K, F, Fs, score, weights):
+    m = Model(D, E, K, F, Fs, score, weights, seed=S + E)
+    x = m.tokens(S)
+    out = m.layer(S)(x)
+    (check_i8 if weights == "i8" else check_bf16)(m, x, out)
+
+
+@pytest.mark.parametrize("D, F", [(8, 8), (24, 1000), (2696, 72)])
+def test_sizes_of_bf16_alone(D, F):
+    m = Model(D, 6, 2, F, Fs=40, seed=D)
+    x = m.tokens(9)
+    check_bf16(m, x, m.layer(9)(x))
+
+
+@pytest.mark.parametrize("weights", ["bf16", "i8"])
+def test_fewer_tokens_than_the_layer_holds(weights):
+    m = Model(144, 12, 3, 176, 64, "sigmoid", weights, seed=3)
+    lf = m.layer(20)
+    x = m.tokens(20)
+    full = {k: v.clone() for k, v in lf(x).items()}
+    for n in (0, 1, 2, 15, 16, 19):
+        for v in lf.out.values():
+            v.fill_(-3)
+        out = lf(x[:n])
+        assert out["y"].shape == (n, 144)
+        assert bool((lf.out["y"][n:] == -3).all()) and bool((lf.out["topk_idx"][n:] == -3).all())
+        assert torch.equal(out["topk_idx"], full["topk_idx"][:n])
+        (check_i8 if weights == "i8" else check_bf16)(m, x[:n], out) if n else None
+
+
+def test_ties_and_masked_experts():
+    m = Model(64, 96, 4, 32, seed=4)
+    m.Wr[:, 40] = m.Wr[:, 7]
+    m.bias[40] = m.bias[7] = 9.0          # 7 and 40 tie at the top
+    x = m.tokens(6)
+    out = m.layer(6)(x)
+    assert bool((out["topk_idx"][:, 0] == 7).all()) and bool((out["topk_idx"][:, 1] == 40).all())
+    assert torch.equal(out["topk_prob"][:, 0], out["topk_prob"][:, 1])
+    # all but K - 1 experts masked: the last pick is the lowest masked one, with weight 0
+    m.bias.fill_(float("-inf"))
+    m.bias[[3, 50, 95]] = 0.0
+    out = m.layer(6)(x)
+    idx = out["topk_idx"].cpu().numpy()
+    assert (np.sort(idx[:, :3], 1) == [3, 50, 95]).all() and (idx[:, 3] == 0).all()
+    assert bool((out["topk_prob"][:, 3] == 0).all())
+    # zero tokens: every expert scores its bias
+    m.bias.zero_()
+    out = m.layer(6)(torch.zeros_like(x))
+    assert (out["topk_idx"].cpu().numpy() == [0, 1, 2, 3]).all() and bool((out["y"] == 0).all())
+    assert bool((out["topk_prob"] == 0.25).all())
+
+
+@pytest.mark.parametrize("weights", ["bf16", "i8"])
+def test_a_token_that_is_not_finite_stays_alone(weights):
+    m = Model(64, 8, 2, 48, seed=5, weights=weights)
+    lf = m.layer(8)
+    x = m.tokens(8)
+    clean = {k: v.clone() for k, v in lf(x).items()}
+    x2 = x.clone()
+    x2[3, 9] = float("inf")
+    out = lf(x2)
+    keep = torch.arange(8, device=DEV) != 3
+    assert not bool(torch.isfinite(out["y"][3]).all())
+    assert torch.equal(out["y"][keep], clean["y"][keep]) and torch.equal(out["topk_idx"][keep], clean["topk_idx"][keep])
+
+
+@pytest.mark.parametrize("weights", ["bf16", "i8"])
+def test_repeats_graphs_streams_and_two_layers(weights):
+    m = Model(528, 20, 4, 272, 144, "sigmoid", weights, seed=6)
+    xs = [m.tokens(11, s) for s in range(3)]
+    lf = m.layer(11)
+    ref = [{k: v.clone() for k, v in lf(x).items()} for x in xs]
+    for x, r in zip(xs, ref):
+        for k, v in lf(x).items():
+            assert torch.equal(v, r[k]), k
+    # two objects of the same weights at once, on two streams
+    other = m.layer(11)
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        with torch.cuda.stream(a):
+            oa = lf(xs[0])
+        with torch.cuda.stream(b):
+            ob = other(xs[1])
+        torch.cuda.synchronize()
+        assert torch.equal(oa["y"], ref[0]["y"]) and torch.equal(ob["y"], ref[1]["y"])
+    # captured, replayed on new values with eager calls between
+    buf = xs[0].clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = lf(buf)
+    for x, r in zip(xs, ref):
+        buf.copy_(x)
+        for v in out.values():
+            v.fill_(-5)
+        graph.replay()
+        torch.cuda.synchronize()
+        for k, v in out.items():
+            assert torch.equal(v, r[k]), k
+        lf(xs[2])
+        torch.cuda.synchronize()
+
+
+def test_follows_the_training_layer():
+    """The same weights and tokens through LayerFwd: the same picks, outputs within both paths' bf16 roundings."""
+    m = Model(256, 16, 4, 512, seed=7)
+    x = m.tokens(64)
+    out = m.layer(64)(x)
+    fwd = layer.LayerFwd(64, 256, 16, 4, 512)(x, m.Wr, m.W1, m.W2, bias=m.bias)
+    assert torch.equal(out["topk_idx"], fwd["topk_idx"])
+    a, b = out["y"].double(), fwd["y"].double()
+    assert float((a - b).norm() / b.norm()) <= 2 * 2.0 ** -8    # three roundings of rms below 2^-9 on one side, two on the other
+    check_bf16(m, x, out)
+
+
+def test_serving_a_model_in_8_bits():
+    """The path as a server runs it: weights quantised once, a prompt through the grouped
+    FFN, then decode steps through the few-token layer; both agree on the last token."""
+    m = Model(256, 16, 4, 512, seed=8, weights="i8")
+    x = m.tokens(300)
+    r = layer.route(layer.router_logits(x, m.Wr, m.bias), m.K)
+    xd, p = layer.dispatch(x, r["topk_prob"], r["inv_perm"], m.K)
+    yd = layer.grouped_ffn_i8(xd, r["offsets"], m.w1, m.s1, m.w2, m.s2)
+    y = layer.combine(yd, p, r["inv_perm"], 300, m.K)
+    lf = m.layer(4)
+    for t in (0, 37, 296):
+        out = lf(x[t:t + 4])
+        assert torch.equal(out["topk_idx"], r["topk_idx"][t:t + 4])
+        d = (out["y"].double() - y[t:t + 4].double()).norm() / y[t:t + 4].double().norm()
+        assert float(d) <= 2 * 2.0 ** -8
+
+
+def test_refusals_on_the_device():
+    m = Model(32, 8, 2, 48)
+    lf = m.layer(4)
+    with pytest.raises(ValueError):
+        lf(m.tokens(5))
+    with pytest.raises(ValueError):
+        lf(torch.zeros(4, 64, dtype=BF16, device=DEV))
+    with pytest.raises(TypeError):
+        lf(torch.zeros(4, 32, device=DEV))
+    with pytest.raises(ValueError):
+        lf(torch.zeros(32, 4, dtype=BF16, device=DEV).t())
+    with pytest.raises(ValueError):
+        m.layer(65)
+    with pytest.raises(ValueError):
+        layer.LayerFew(4, m.Wr, m.W1, m.W2, 2, sel_bias=m.bias, score="softmax")
