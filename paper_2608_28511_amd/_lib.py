@@ -185,11 +185,21 @@ def _ptr(t: Optional[torch.Tensor], dtype=None, name: str = "tensor"):
 
 
 def _here(t: Optional[torch.Tensor], dtype=None, name: str = "tensor"):
-    """_ptr of a tensor on the current device, whose stream the call goes to."""
+    """Address of a tensor on the current device, whose stream the call goes to; checked as _ptr does."""
+    if t is None:
+        return None
+    if (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous() and (dtype is None or t.dtype is dtype)
+            and t.get_device() == torch._C._cuda_getDevice()):
+        return t.data_ptr()
     p = _ptr(t, dtype, name)
-    if p is not None and t.device.index != torch.cuda.current_device():
+    if p is not None:
         raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
     return p
+
+
+def _raw_stream():
+    """_stream() without the objects around it."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 BF16, F32, I32, I8 = torch.bfloat16, torch.float32, torch.int32, torch.int8
@@ -481,18 +491,18 @@ def moe_grouped_gemm_mxfp8(x_q, x_scale, sched, E, R, Kd, N, W, epilogue, Cout, 
 
 def moe_quant_rows_i8(x, R, D, q, scale):
     _check(load().moe_quant_rows_i8(_here(x, BF16, "x"), R, D, _here(q, I8, "q"), _here(scale, F32, "scale"),
-                                    _stream()), "moe_quant_rows_i8")
+                                    _raw_stream()), "moe_quant_rows_i8")
 
 
 def moe_quant_weights_i8(W, E, Kd, N, Wq, scale):
     _check(load().moe_quant_weights_i8(_here(W, BF16, "W"), E, Kd, N, _here(Wq, I8, "Wq"),
-                                       _here(scale, F32, "scale"), _stream()), "moe_quant_weights_i8")
+                                       _here(scale, F32, "scale"), _raw_stream()), "moe_quant_weights_i8")
 
 
 def moe_grouped_gemm_i8(Aq, a_scale, sched, E, R, Kd, N, Wq, w_scale, epilogue, Cout):
     _check(load().moe_grouped_gemm_i8(
         _here(Aq, I8, "Aq"), _here(a_scale, F32, "a_scale"), _here(sched, None, "sched"), E, R, Kd, N,
-        _here(Wq, I8, "Wq"), _here(w_scale, F32, "w_scale"), epilogue, _here(Cout, BF16, "C"), _stream()),
+        _here(Wq, I8, "Wq"), _here(w_scale, F32, "w_scale"), epilogue, _here(Cout, BF16, "C"), _raw_stream()),
         "moe_grouped_gemm_i8")
 
 
@@ -503,7 +513,7 @@ def moe_latent_proj_i8_workspace_bytes(M, Kd) -> int:
 def moe_latent_proj_i8(A, Wq, w_scale, M, Kd, N, Cout, ws):
     _check(load().moe_latent_proj_i8(
         _here(A, BF16, "A"), _here(Wq, I8, "Wq"), _here(w_scale, F32, "w_scale"), M, Kd, N, _here(Cout, BF16, "C"),
-        _here(ws, None, "ws"), _wsz(ws), _stream()), "moe_latent_proj_i8")
+        _here(ws, None, "ws"), _wsz(ws), _raw_stream()), "moe_latent_proj_i8")
 
 
 def moe_grouped_ffn_i8_workspace_bytes(E, R, D, F) -> int:
@@ -514,7 +524,7 @@ def moe_grouped_ffn_i8(x_disp, offsets, E, R, D, F, W1q, s1, W2q, s2, y_disp, ws
     _check(load().moe_grouped_ffn_i8(
         _here(x_disp, BF16, "x_disp"), _here(offsets, I32, "offsets"), E, R, D, F, _here(W1q, I8, "W1q"),
         _here(s1, F32, "s1"), _here(W2q, I8, "W2q"), _here(s2, F32, "s2"), _here(y_disp, BF16, "y_disp"),
-        _here(ws, None, "ws"), _wsz(ws), _stream()), "moe_grouped_ffn_i8")
+        _here(ws, None, "ws"), _wsz(ws), _raw_stream()), "moe_grouped_ffn_i8")
 
 
 _FEW_TENSORS = {"x": BF16, "Wr": F32, "router_bias": F32, "sel_bias": F32, "s1": F32, "s2": F32, "ss1": F32,
@@ -547,4 +557,4 @@ def moe_layer_few_workspace_bytes(args: LayerFewArgs) -> int:
 
 
 def moe_layer_few(args: LayerFewArgs):
-    _check(load().moe_layer_few(C.byref(args), _stream()), "moe_layer_few")
+    _check(load().moe_layer_few(C.byref(args), _raw_stream()), "moe_layer_few")

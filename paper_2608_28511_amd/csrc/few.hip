@@ -5,17 +5,18 @@
 // permutation is built: routed row r = t K + k keeps its place, and a workgroup of a
 // product finds its expert and that expert's rows in the S K picks itself.
 //
-//   few_logits   partial router logits: 64 d x 64 experts a workgroup, fp32 products
+//   few_logits   partial router logits: 64 d x 64 experts x 16 tokens a workgroup, fp32 products
 //   few_route    one workgroup a token: the partial sums, top-K and weights; with 8-bit
 //                weights as many again quantise the token rows
-//   few_gemm     up: partial u = x W1 over a share of the contraction
-//   few_act      h = bf16(max(u, 0)^2) (8-bit weights: and its rows' codes)
-//   few_gemm     down: partial y = h W2
+//   few_gemm     up: h = bf16(max(x W1, 0)^2)
+//   few_quant    8-bit weights: the rows of h
+//   few_gemm     down: y_k = h W2 in fp32
 //   few_combine  y = bf16(sum_k p_k y_k + shared), all sums in fp32 and fixed order
 //
 // few_gemm's matrix products take 16 tokens; weights go from memory to the matrix
-// cores' operands in registers, each wave a share of the contraction, several
-// steps ahead, and never through LDS: every weight is used by one wave only.
+// cores' operands in registers, several steps ahead, and never through LDS: every
+// weight is used by one wave only.  The waves of a workgroup share a slab of output
+// columns, each a part of its contraction.
 #include <algorithm>
 
 #include "kernels.h"
@@ -36,24 +37,25 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t few_rsrc(const void* base, int
 // ---- router ---------------------------------------------------------------
 // part[chunk][t][e] = sum over 64 d of x[t, d] Wr[d, e].  A lane is an expert and a
 // wave 16 of the 64 d, whose weights it holds; token values are broadcast from LDS.
-constexpr int kFewD = 64;
+constexpr int kFewD = 64, kFewT = 16;
 __global__ __launch_bounds__(kFewThreads) void few_logits_kernel(const uint16_t* __restrict__ x,
                                                                  const float* __restrict__ Wr, int S, int D, int E,
                                                                  float* __restrict__ part) {
-    __shared__ float xs[kFewMaxTokens][kFewD];
-    __shared__ float red[4][kFewMaxTokens][64];
+    __shared__ float xs[kFewT][kFewD];
+    __shared__ float red[4][kFewT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int d0 = blockIdx.x * kFewD, e = blockIdx.y * 64 + lane;
+    const int t0 = blockIdx.z * kFewT, nt = S - t0 < kFewT ? S - t0 : kFewT;
     float w[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const int d = d0 + wave * 16 + i;
         w[i] = d < D && e < E ? Wr[(int64_t)d * E + e] : 0.f;
     }
-    for (int c = threadIdx.x; c < S * (kFewD / 8); c += kFewThreads) {
+    for (int c = threadIdx.x; c < nt * (kFewD / 8); c += kFewThreads) {
         const int t = c / (kFewD / 8), d = (c % (kFewD / 8)) * 8;
         uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (d0 + d < D) v = *(const uint4*)(x + (int64_t)t * D + d0 + d);   // D is a multiple of 8
+        if (d0 + d < D) v = *(const uint4*)(x + (int64_t)(t0 + t) * D + d0 + d);   // D is a multiple of 8
         const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -62,7 +64,7 @@ __global__ __launch_bounds__(kFewThreads) void few_logits_kernel(const uint16_t*
         }
     }
     __syncthreads();
-    for (int t = 0; t < S; ++t) {
+    for (int t = 0; t < nt; ++t) {
         float a = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) a = fmaf(xs[t][wave * 16 + i], w[i], a);
@@ -70,8 +72,8 @@ __global__ __launch_bounds__(kFewThreads) void few_logits_kernel(const uint16_t*
     }
     __syncthreads();
     if (e >= E) return;
-    for (int t = wave; t < S; t += 4)
-        part[((int64_t)blockIdx.x * S + t) * E + e] =
+    for (int t = wave; t < nt; t += 4)
+        part[((int64_t)blockIdx.x * S + t0 + t) * E + e] =
             (red[0][t][lane] + red[1][t][lane]) + (red[2][t][lane] + red[3][t][lane]);
 }
 
@@ -178,16 +180,20 @@ __global__ __launch_bounds__(kFewThreads) void few_route_kernel(
 struct FewSide {
     const void* A;       // rows of lda bytes; routed row r reads row r / a_div
     const void* W;       // bf16 [Kd, N] or int8 [N, Kd] per expert
-    uint32_t* out;       // [splits][rows][N] fp32 or int32
+    void* out;           // [rows][N]: h in bf16 (up) or y in fp32 (down)
+    const float* row_scale;     // 8-bit: of A's rows
+    const float* col_scale;     // 8-bit: [experts][N]
     int64_t a_bytes, w_bytes;   // of A, of one expert's W
     int lda, a_div;
-    int Kd, N, rows;
-    int slabs, splits;   // output columns and contraction in this many workgroups
+    int Kd, N;
+    int groups;          // workgroups an expert takes
 };
 struct FewGemmArgs {
     FewSide routed, shared;
     const int32_t* idx;   // [S, K]
     int S, K, r_items;    // workgroups of the routed experts
+    int wk;               // waves that share a slab's contraction; 4 / wk slabs side by side in a workgroup
+    int up;
 };
 
 // The a-th expert (ascending) among the n picks and its rows, in order, in rows[];
@@ -231,11 +237,11 @@ __device__ __forceinline__ int few_plan(const int32_t* __restrict__ idx, int n, 
     return e;
 }
 
-// bf16 weights, N-contiguous: a workgroup's 64 columns, a wave's every fourth step of
-// 32 k.  A lane loads 4 columns of 8 k rows (each load of the wave four whole cache
-// lines) and packs them into the fragments of columns 4 c + q, q = 0 .. 3, with one byte
-// permutation a register.
+// bf16 weights, N-contiguous: slabs of 64 columns, steps of 32 k.  A lane loads 4
+// columns of 8 k rows (each load of the wave four whole cache lines) and packs them into
+// the fragments of columns 4 c + q, q = 0 .. 3, with one byte permutation a register.
 struct FewBf16 {
+    static constexpr bool kI8 = false;
     static constexpr int kCols = 64, kStep = 32, kAcc = 4;
     template <int MB>
     static constexpr int kAhead = MB == 4 ? 3 : 4;
@@ -272,21 +278,20 @@ struct FewBf16 {
                 acc[m][q] = mfma16<false>(__builtin_bit_cast(bf16x8, f), __builtin_bit_cast(bf16x8, a.v[m]), acc[m][q]);
         }
     }
-    // acc[q][v] of a lane is column 16 g + 4 v + q of its token: four stores of four columns
-    template <class T>
-    __device__ __forceinline__ static void leave(const f32x4 (&acc)[kAcc], T&& put, int lane) {
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-            put(16 * (lane >> 4) + 4 * v, f32x4{acc[0][v], acc[1][v], acc[2][v], acc[3][v]});
+    // acc[q][v] of a lane is column 16 g + 4 v + q of its token: piece v is four columns
+    __device__ __forceinline__ static f32x4 piece(const f32x4 (&acc)[kAcc], int v) {
+        return f32x4{acc[0][v], acc[1][v], acc[2][v], acc[3][v]};
     }
+    __device__ __forceinline__ static int piece_col(int v, int lane) { return 16 * (lane >> 4) + 4 * v; }
 };
 
-// 8-bit weights, K-contiguous: a workgroup's 32 columns, a wave's every fourth step of
-// 128 k, whose fragments are 16 bytes of a channel as they lie in memory.
+// 8-bit weights, K-contiguous: slabs of 32 columns, steps of 128 k, whose fragments
+// are 16 bytes of a channel as they lie in memory.
 struct FewI8 {
+    static constexpr bool kI8 = true;
     static constexpr int kCols = 32, kStep = 128, kAcc = 2;
     template <int MB>
-    static constexpr int kAhead = MB == 4 ? 2 : 4;
+    static constexpr int kAhead = MB == 4 ? 2 : 3;
     u32x4 w[2][2];
 
     __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t& rw, const FewSide& s, int n0, int k, int lane) {
@@ -326,24 +331,29 @@ struct FewI8 {
                     acc[m][b] = mfma16<true>(__builtin_bit_cast(bf16x8, w[b][h]), __builtin_bit_cast(bf16x8, a.v[m][h]),
                                              acc[m][b]);
     }
-    template <class T>
-    __device__ __forceinline__ static void leave(const f32x4 (&acc)[kAcc], T&& put, int lane) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b) put(16 * b + 4 * (lane >> 4), acc[b]);
-    }
+    __device__ __forceinline__ static f32x4 piece(const f32x4 (&acc)[kAcc], int b) { return acc[b]; }
+    __device__ __forceinline__ static int piece_col(int b, int lane) { return 16 * b + 4 * (lane >> 4); }
 };
 
-// The workgroup's partial product for 16 MB rows: steps [st0, st1), the waves' sums
-// joined in LDS in wave order.
+template <bool I8>
+__device__ __forceinline__ f32x4 few_add(f32x4 a, f32x4 b) {
+    if constexpr (I8)
+        return __builtin_bit_cast(f32x4, __builtin_bit_cast(i32x4, a) + __builtin_bit_cast(i32x4, b));
+    else
+        return a + b;
+}
+
+// Columns [n0, n0 + kCols) of the product for 16 MB rows of expert e.  The wave is the
+// kk-th of the wk that share the slab: it takes every wk-th step, and their sums are
+// joined through LDS in wave order, each wave finishing some of the slab's pieces.
+// Every wave of the workgroup calls it (n0 may lie past N: such a slab has nothing to do).
 template <class T, int MB>
-__device__ __forceinline__ void few_body(const FewSide& s, int e, int n0, int split, const int32_t* rows, int nrows,
-                                         uint32_t (*red)[16][T::kCols + 4]) {
-    constexpr bool I8 = std::is_same<T, FewI8>::value;
+__device__ __forceinline__ void few_body(const FewGemmArgs& p, const FewSide& s, int e, int n0, int kk, int wk,
+                                         const int32_t* rows, int nrows, f32x4 (*red)[T::kAcc][64]) {
     constexpr int P = T::template kAhead<MB>;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int nst = (s.Kd + T::kStep - 1) / T::kStep;
-    const int st0 = (int)((int64_t)nst * split / s.splits), st1 = (int)((int64_t)nst * (split + 1) / s.splits);
-    const int mine = st1 - st0 > wave ? (st1 - st0 - wave + 3) / 4 : 0;
+    const int mine = n0 < s.N && nst > kk ? (nst - kk + wk - 1) / wk : 0;
     const __amdgpu_buffer_rsrc_t rw = few_rsrc((const char*)s.W + e * s.w_bytes, s.w_bytes);
     const __amdgpu_buffer_rsrc_t ra = few_rsrc(s.A, s.a_bytes);
     uint32_t row[MB];
@@ -360,7 +370,7 @@ __device__ __forceinline__ void few_body(const FewSide& s, int e, int n0, int sp
     T w[P];
     typename T::template A<MB> a[P];
     auto load = [&](int slot, int i) {
-        const int k = (st0 + wave + 4 * i) * T::kStep;
+        const int k = (kk + wk * i) * T::kStep;
         w[slot].load(rw, s, n0, k, lane);
         a[slot].load(ra, row, k, s.Kd, lane);
     };
@@ -375,40 +385,59 @@ __device__ __forceinline__ void few_body(const FewSide& s, int e, int n0, int sp
             if (i0 + q + P < mine) load(q, i0 + q + P);
         }
     }
+    auto leave = [&](int m, int v, f32x4 t) {
+        const int i = m * 16 + (lane & 15), col = n0 + T::piece_col(v, lane);
+        if (i >= nrows || col >= s.N) return;   // N is a multiple of 8
+        const int r = rows[i];
+        if constexpr (T::kI8) {
+            const float rs = s.row_scale[r / s.a_div];
+            const f32x4 cs = *(const f32x4*)(s.col_scale + (int64_t)e * s.N + col);
 #pragma unroll
-    for (int m = 0; m < MB; ++m) {
-        if (m > 0) __syncthreads();
-        T::leave(acc[m], [&](int col, f32x4 v) { *(f32x4*)&red[wave][lane & 15][col] = v; }, lane);
-        __syncthreads();
-        for (int c = tid; c < 16 * (T::kCols / 4); c += kFewThreads) {
-            const int i = c / (T::kCols / 4), col = (c % (T::kCols / 4)) * 4;
-            if (m * 16 + i >= nrows || n0 + col >= s.N) continue;   // N is a multiple of 8
-            u32x4 v[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) v[u] = *(const u32x4*)&red[u][i][col];
-            u32x4 t;
+            for (int q = 0; q < 4; ++q) t[q] = (float)__float_as_int(t[q]) * rs * cs[q];
+        }
+        const int64_t at = (int64_t)r * s.N + col;
+        if (p.up) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                if constexpr (I8)
-                    t[q] = (v[0][q] + v[1][q]) + (v[2][q] + v[3][q]);
-                else
-                    t[q] = __float_as_uint((__uint_as_float(v[0][q]) + __uint_as_float(v[1][q])) +
-                                           (__uint_as_float(v[2][q]) + __uint_as_float(v[3][q])));
+                t[q] = relu_f32(t[q]);
+                t[q] *= t[q];
             }
-            *(u32x4*)(s.out + ((int64_t)split * s.rows + rows[m * 16 + i]) * s.N + n0 + col) = t;
+            *(u32x2*)((uint16_t*)s.out + at) = u32x2{pack_bf16x2(t[0], t[1]), pack_bf16x2(t[2], t[3])};
+        } else {
+            *(f32x4*)((float*)s.out + at) = t;
+        }
+    };
+#pragma unroll
+    for (int m = 0; m < MB; ++m) {
+        if (m > 0 && m * 16 >= nrows) break;
+        if (wk == 1) {
+#pragma unroll
+            for (int v = 0; v < T::kAcc; ++v) leave(m, v, T::piece(acc[m], v));
+        } else {
+            if (m > 0) __syncthreads();
+#pragma unroll
+            for (int v = 0; v < T::kAcc; ++v) red[wave][v][lane] = T::piece(acc[m], v);
+            __syncthreads();
+            const int first = wave - kk;
+            for (int v = kk; v < T::kAcc; v += wk) {
+                f32x4 t = red[first][v][lane];
+                for (int j = 1; j < wk; ++j) t = few_add<T::kI8>(t, red[first + j][v][lane]);
+                leave(m, v, t);
+            }
         }
     }
 }
 
-template <class T>
-__global__ __launch_bounds__(kFewThreads, 2) void few_gemm_kernel(FewGemmArgs p) {
+// MBMAX = 1: at most 16 tokens, so at most 16 rows an expert; four waves a SIMD.
+template <class T, int MBMAX>
+__global__ __launch_bounds__(kFewThreads, MBMAX == 1 ? 4 : 2) void few_gemm_kernel(FewGemmArgs p) {
     __shared__ uint32_t seen[32];
-    __shared__ int32_t picks[kFewMaxTokens * 32], rows[kFewMaxTokens], nrows_s;
-    __shared__ __attribute__((aligned(16))) uint32_t red[4][16][T::kCols + 4];
+    __shared__ int32_t picks[(MBMAX == 1 ? 16 : kFewMaxTokens) * 32], rows[kFewMaxTokens], nrows_s;
+    __shared__ f32x4 red[4][T::kAcc][64];   // wk > 1: every wave's sums
     const bool shared = (int)blockIdx.x >= p.r_items;
     const int b = (int)blockIdx.x - (shared ? p.r_items : 0);
     const FewSide s = shared ? p.shared : p.routed;
-    const int a = b / (s.slabs * s.splits), in = b - a * (s.slabs * s.splits);
+    const int a = b / s.groups, in = b - a * s.groups;
     int e = 0;
     if (shared) {
         if ((int)threadIdx.x < p.S) rows[threadIdx.x] = threadIdx.x;
@@ -419,120 +448,92 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_gemm_kernel(FewGemmArgs p)
     }
     __syncthreads();
     const int nrows = __builtin_amdgcn_readfirstlane(nrows_s);
-    const int split = in / s.slabs, n0 = (in - split * s.slabs) * T::kCols;
-    if (nrows <= 16) few_body<T, 1>(s, e, n0, split, rows, nrows, red);
-    else if (nrows <= 32) few_body<T, 2>(s, e, n0, split, rows, nrows, red);
-    else few_body<T, 4>(s, e, n0, split, rows, nrows, red);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wk = p.wk;
+    const int kk = wave & (wk - 1), wn = wave / wk;
+    const int n0 = (in * (4 / wk) + wn) * T::kCols;
+    if (MBMAX == 1 || nrows <= 16) few_body<T, 1>(p, s, e, n0, kk, wk, rows, nrows, red);
+    else if (nrows <= 32) few_body<T, MBMAX == 1 ? 1 : 2>(p, s, e, n0, kk, wk, rows, nrows, red);
+    else few_body<T, MBMAX == 1 ? 1 : 4>(p, s, e, n0, kk, wk, rows, nrows, red);
 }
 
 // ---- between the products and after them ------------------------------------
-struct FewAct {
-    const uint32_t* u;       // [splits][rows][F]
-    void* h;                 // [rows][F] bf16 or int8
-    float* hs;               // [rows] scales (8-bit)
-    const float* scale;      // [experts][F] channel scales (8-bit)
-    int F, rows, splits;
+struct FewRows {
+    const uint16_t* h;   // [rows][F]
+    int8_t* q;
+    float* scale;
+    int F, rows;
 };
 
-// Four elements of the row's activation from the partial sums.
-template <bool I8>
-__device__ __forceinline__ void few_act4(const FewAct& p, int row, int f, float xs, const float* cs, uint32_t& h01,
-                                         uint32_t& h23) {
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
-    int n[4] = {0, 0, 0, 0};
-    for (int s = 0; s < p.splits; ++s) {
-        const u32x4 w = *(const u32x4*)(p.u + ((int64_t)s * p.rows + row) * p.F + f);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if constexpr (I8) n[q] += (int)w[q];
-            else v[q] += __uint_as_float(w[q]);
-        }
-    }
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        if constexpr (I8) v[q] = (float)n[q] * xs * cs[f + q];
-        v[q] = relu_f32(v[q]);
-        v[q] *= v[q];
-    }
-    h01 = pack_bf16x2(v[0], v[1]);
-    h23 = pack_bf16x2(v[2], v[3]);
-}
-
-// One workgroup a row: routed rows first, then the shared expert's.
-template <bool I8>
-__global__ __launch_bounds__(kFewThreads) void few_act_kernel(FewAct routed, FewAct shared,
-                                                              const int32_t* __restrict__ idx,
-                                                              const float* __restrict__ xs, int K) {
+// 8-bit rows of the activations, one workgroup a row: the routed experts', then the
+// shared one's.
+__global__ __launch_bounds__(kFewThreads) void few_quant_kernel(FewRows routed, FewRows shared) {
     __shared__ uint32_t tops[4];
     const bool sh = (int)blockIdx.x >= routed.rows;
-    const FewAct p = sh ? shared : routed;
-    const int row = (int)blockIdx.x - (sh ? routed.rows : 0);
+    const FewRows p = sh ? shared : routed;
+    const int64_t row = (int)blockIdx.x - (sh ? routed.rows : 0);
     const int tid = threadIdx.x;
-    float x = 1.f;
-    const float* cs = nullptr;
-    if constexpr (I8) {
-        x = xs[sh ? row : row / K];
-        cs = p.scale + (sh ? 0 : (int64_t)idx[row] * p.F);
-    }
+    const uint4* src = (const uint4*)(p.h + row * p.F);
+    uint2* dst = (uint2*)(p.q + row * p.F);
+    const int n = p.F / 8;
+    uint4 v[2];   // the row's first 4,096 elements stay in registers
     uint32_t top = 0;
-    for (int f = tid * 4; f < p.F; f += kFewThreads * 4) {
-        uint32_t a, b;
-        few_act4<I8>(p, row, f, x, cs, a, b);
-        if constexpr (I8) top = max_mag(max_mag(top, a), b);
-        else *(uint2*)((uint16_t*)p.h + (int64_t)row * p.F + f) = make_uint2(a, b);
+    for (int i = 0; i * kFewThreads < n; ++i) {
+        const int c = tid + i * kFewThreads;
+        const uint4 u = c < n ? src[c] : make_uint4(0u, 0u, 0u, 0u);
+        if (i == 0) v[0] = u;
+        if (i == 1) v[1] = u;
+        top = max_mag(max_mag(max_mag(max_mag(top, u.x), u.y), u.z), u.w);
     }
-    if constexpr (I8) {
-        top = wave_max_u32(top);
-        if ((tid & 63) == 0) tops[tid >> 6] = top;
-        __syncthreads();
-        Quant8 s;
-        s.init(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
-        if (tid == 0) p.hs[row] = s.scale;
-        for (int f = tid * 4; f < p.F; f += kFewThreads * 4) {
-            uint32_t a, b;
-            few_act4<I8>(p, row, f, x, cs, a, b);
-            *(uint32_t*)((int8_t*)p.h + (int64_t)row * p.F + f) = codes4(s, a, b);
-        }
-    }
-}
-
-struct FewOut {
-    const uint32_t* y;     // [splits][rows][D] partial products
-    const float* hs;       // [rows] (8-bit)
-    const float* scale;    // [experts][D] (8-bit)
-    int rows, splits;
-};
-
-template <bool I8>
-__device__ __forceinline__ void few_out4(const FewOut& p, int row, int64_t e, int D, int d, float w, float (&y)[4]) {
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
-    int n[4] = {0, 0, 0, 0};
-    for (int s = 0; s < p.splits; ++s) {
-        const u32x4 q4 = *(const u32x4*)(p.y + ((int64_t)s * p.rows + row) * D + d);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if constexpr (I8) n[q] += (int)q4[q];
-            else v[q] += __uint_as_float(q4[q]);
-        }
-    }
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        if constexpr (I8) v[q] = (float)n[q] * p.hs[row] * p.scale[e * D + d + q];
-        y[q] = fmaf(w, v[q], y[q]);
+    top = wave_max_u32(top);
+    if ((tid & 63) == 0) tops[tid >> 6] = top;
+    __syncthreads();
+    Quant8 s;
+    s.init(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
+    if (tid == 0) p.scale[row] = s.scale;
+    for (int i = 0; i * kFewThreads < n; ++i) {
+        const int c = tid + i * kFewThreads;
+        if (c >= n) break;
+        const uint4 u = i == 0 ? v[0] : i == 1 ? v[1] : src[c];
+        dst[c] = make_uint2(codes4(s, u.x, u.y), codes4(s, u.z, u.w));
     }
 }
 
-template <bool I8>
-__global__ __launch_bounds__(64) void few_combine_kernel(FewOut routed, FewOut shared, const int32_t* __restrict__ idx,
-                                                         const float* __restrict__ prob, int K, int D,
-                                                         uint16_t* __restrict__ y) {
-    const int t = blockIdx.y, d = (blockIdx.x * 64 + threadIdx.x) * 4;
-    if (d >= D) return;
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < K; ++k)
-        few_out4<I8>(routed, t * K + k, I8 ? idx[t * K + k] : 0, D, d, prob[t * K + k], v);
-    if (shared.rows > 0) few_out4<I8>(shared, t, 0, D, d, 1.f, v);
-    *(uint2*)(y + (int64_t)t * D + d) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+// Sixty-four groups of four columns a workgroup; a wave takes every fourth expert of
+// the token's K, so that at most eight loads follow each other, and the waves' sums are
+// added in order.
+__global__ __launch_bounds__(kFewThreads) void few_combine_kernel(const float* __restrict__ yk,
+                                                                  const float* __restrict__ ys,
+                                                                  const float* __restrict__ prob, int K, int D,
+                                                                  uint16_t* __restrict__ y) {
+    __shared__ f32x4 sum[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int t = blockIdx.y, d = (blockIdx.x * 64 + lane) * 4;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (d < D) {
+        f32x4 u[8];
+        float w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int k = wave + 4 * i;
+            w[i] = 0.f;
+            if (k < K) {
+                w[i] = prob[t * K + k];
+                u[i] = *(const f32x4*)(yk + (int64_t)(t * K + k) * D + d);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (wave + 4 * i < K) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) v[q] = fmaf(w[i], u[i][q], v[q]);
+            }
+        if (wave == 3 && ys != nullptr) v += *(const f32x4*)(ys + (int64_t)t * D + d);
+    }
+    sum[wave][lane] = v;
+    __syncthreads();
+    if (wave != 0 || d >= D) return;
+    v = ((sum[0][lane] + sum[1][lane]) + sum[2][lane]) + sum[3][lane];
+    *(u32x2*)(y + (int64_t)t * D + d) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
 }
 
 // ---- host -------------------------------------------------------------------
@@ -540,22 +541,22 @@ namespace {
 
 size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 
-struct FewPlan {
-    int nd, r_experts;
-    int cols, step;
-    int slabs1, slabs2, slabs1s;           // 64- or 32-column slabs of F, D, Fs
-    int split1, split2, split2s;           // shares of D (both up products), F, Fs
-    size_t part, idx, prob, xq, xs, u, us, h, hs, hsc, hssc, y, ys, bytes;   // offsets
-};
-
 int cdiv(int a, int b) { return (a + b - 1) / b; }
 
-// Shares of a contraction of `steps` steps: enough workgroups for two a compute unit,
-// while every wave keeps two steps.
-int few_splits(int items, int steps) {
-    const int want = cdiv(2 * cu_count(), items > 0 ? items : 1);
-    const int most = std::max(1, steps / 8);
-    return std::max(1, std::min(want, most));
+struct FewPlan {
+    int nd, r_experts;
+    int wk1, wk2;          // waves that share a slab of the up and of the down product
+    size_t part, idx, prob, xq, xs, h, hs, hq, hqs, sc, scs, y, ys, bytes;   // offsets
+};
+
+// Waves of a workgroup's four that share a slab's contraction, each keeping a step.  Four
+// give the most workgroups, which the CUs then share evenly (us with 1 / 2 / 4, one product's
+// choice varied: 8 tokens of 192 experts 382 / 354 / 347; 1 token of 64 40 / 31 / 26.5); with many
+// picks two, since every workgroup searches them all (64 tokens of 64 experts: 116 / 119 / 121
+// and 119 / 120 / 127; 32 of 256: 302 / 290 / 283 and 303 / 300 / 314).
+int few_share(int picks, int steps) {
+    const int most = picks > 256 ? 2 : 4;
+    return std::min(most, steps >= 4 ? 4 : steps >= 2 ? 2 : 1);
 }
 
 FewPlan few_plan_of(const moe_layer_few_args* a) {
@@ -563,17 +564,11 @@ FewPlan few_plan_of(const moe_layer_few_args* a) {
     const int S = (int)a->S, D = a->D, E = a->E, K = a->K, F = a->F, Fs = a->Fs;
     const bool i8 = a->weights == MOE_WEIGHTS_I8;
     const size_t R = (size_t)S * K;
+    const int step = i8 ? FewI8::kStep : FewBf16::kStep;
     p.nd = cdiv(D, kFewD);
     p.r_experts = (int)std::min<size_t>((size_t)E, R);
-    p.cols = i8 ? FewI8::kCols : FewBf16::kCols;
-    p.step = i8 ? FewI8::kStep : FewBf16::kStep;
-    p.slabs1 = cdiv(F, p.cols);
-    p.slabs2 = cdiv(D, p.cols);
-    p.slabs1s = cdiv(Fs, p.cols);
-    p.split1 = few_splits(p.r_experts * p.slabs1 + p.slabs1s, cdiv(D, p.step));
-    const int items2 = (p.r_experts + (Fs ? 1 : 0)) * p.slabs2;
-    p.split2 = few_splits(items2, cdiv(F, p.step));
-    p.split2s = Fs ? few_splits(items2, cdiv(Fs, p.step)) : 1;
+    p.wk1 = few_share((int)R, cdiv(D, step));
+    p.wk2 = few_share((int)R, cdiv(F, step));
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t o = at;
@@ -585,14 +580,14 @@ FewPlan few_plan_of(const moe_layer_few_args* a) {
     p.prob = take(R * 4);
     p.xq = take(i8 ? (size_t)S * D : 0);
     p.xs = take((size_t)S * 4);
-    p.u = take((size_t)p.split1 * R * F * 4);
-    p.us = take((size_t)p.split1 * S * Fs * 4);
-    p.h = take(R * F * (i8 ? 1 : 2));
-    p.hs = take((size_t)S * Fs * (i8 ? 1 : 2));
-    p.hsc = take(R * 4);
-    p.hssc = take((size_t)S * 4);
-    p.y = take((size_t)p.split2 * R * D * 4);
-    p.ys = take(Fs ? (size_t)p.split2s * S * D * 4 : 0);
+    p.h = take(R * F * 2);
+    p.hs = take((size_t)S * Fs * 2);
+    p.hq = take(i8 ? R * F : 0);
+    p.hqs = take(i8 ? (size_t)S * Fs : 0);
+    p.sc = take(R * 4);
+    p.scs = take((size_t)S * 4);
+    p.y = take(R * D * 4);
+    p.ys = take(Fs ? (size_t)S * D * 4 : 0);
     p.bytes = at;
     return p;
 }
@@ -616,19 +611,18 @@ hipError_t launch_layer_few(const moe_layer_few_args* a, hipStream_t st) {
     const FewPlan p = few_plan_of(a);
     const int S = (int)a->S, D = a->D, E = a->E, K = a->K, F = a->F, Fs = a->Fs, R = S * K;
     const bool i8 = a->weights == MOE_WEIGHTS_I8;
-    const int wb = i8 ? 1 : 2;
+    const int wb = i8 ? 1 : 2, cols = i8 ? FewI8::kCols : FewBf16::kCols;
     char* ws = (char*)a->ws;
     float* part = (float*)(ws + p.part);
     int32_t* idx = a->topk_idx != nullptr ? a->topk_idx : (int32_t*)(ws + p.idx);
     float* prob = a->topk_prob != nullptr ? a->topk_prob : (float*)(ws + p.prob);
-    int8_t* xq = (int8_t*)(ws + p.xq);
-    float *xs = (float*)(ws + p.xs), *hsc = (float*)(ws + p.hsc), *hssc = (float*)(ws + p.hssc);
-    uint32_t *u = (uint32_t*)(ws + p.u), *us = (uint32_t*)(ws + p.us);
-    uint32_t *y = (uint32_t*)(ws + p.y), *ys = (uint32_t*)(ws + p.ys);
-    void *h = ws + p.h, *hs = ws + p.hs;
+    int8_t *xq = (int8_t*)(ws + p.xq), *hq = (int8_t*)(ws + p.hq), *hqs = (int8_t*)(ws + p.hqs);
+    float *xs = (float*)(ws + p.xs), *sc = (float*)(ws + p.sc), *scs = (float*)(ws + p.scs);
+    uint16_t *h = (uint16_t*)(ws + p.h), *hs = (uint16_t*)(ws + p.hs);
+    float *y = (float*)(ws + p.y), *ys = (float*)(ws + p.ys);
 
-    hipLaunchKernelGGL(few_logits_kernel, dim3((unsigned)p.nd, (unsigned)cdiv(E, 64)), dim3(kFewThreads), 0, st, a->x,
-                       a->Wr, S, D, E, part);
+    hipLaunchKernelGGL(few_logits_kernel, dim3((unsigned)p.nd, (unsigned)cdiv(E, 64), (unsigned)cdiv(S, kFewT)),
+                       dim3(kFewThreads), 0, st, a->x, a->Wr, S, D, E, part);
     const dim3 gr((unsigned)(i8 ? 2 * S : S));
     const bool sig = a->score_fn == MOE_SCORE_SIGMOID;
     if (E <= 64) launch_route_few<1>(sig, gr, st, part, p.nd, a, idx, prob, xq, xs);
@@ -637,35 +631,38 @@ hipError_t launch_layer_few(const moe_layer_few_args* a, hipStream_t st) {
     else if (E <= 512) launch_route_few<8>(sig, gr, st, part, p.nd, a, idx, prob, xq, xs);
     else launch_route_few<16>(sig, gr, st, part, p.nd, a, idx, prob, xq, xs);
 
-    auto side = [&](const void* A, int64_t a_rows, int a_div, const void* W, int Kd, int N, int rows, int slabs,
-                    int splits, uint32_t* out) {
-        FewSide s{};
-        s.A = A; s.W = W; s.out = out;
-        s.lda = Kd * wb;
-        s.a_bytes = a_rows * s.lda;
-        s.w_bytes = (int64_t)Kd * N * wb;
-        s.a_div = a_div; s.Kd = Kd; s.N = N; s.rows = rows; s.slabs = slabs; s.splits = splits;
-        return s;
+    auto gemm = [&](FewSide r, FewSide s, int wk, bool up) {
+        for (FewSide* q : {&r, &s}) {
+            q->lda = q->Kd * wb;
+            q->a_bytes *= q->lda;                       // given as rows
+            q->w_bytes = (int64_t)q->Kd * q->N * wb;
+            q->groups = cdiv(cdiv(q->N, cols), 4 / wk);
+        }
+        const FewGemmArgs g{r, s, idx, S, K, p.r_experts * r.groups, wk, up ? 1 : 0};
+        const dim3 grid((unsigned)(g.r_items + (Fs ? s.groups : 0))), block(kFewThreads);
+        if (S <= 16) {
+            if (i8) hipLaunchKernelGGL((few_gemm_kernel<FewI8, 1>), grid, block, 0, st, g);
+            else hipLaunchKernelGGL((few_gemm_kernel<FewBf16, 1>), grid, block, 0, st, g);
+        } else {
+            if (i8) hipLaunchKernelGGL((few_gemm_kernel<FewI8, 4>), grid, block, 0, st, g);
+            else hipLaunchKernelGGL((few_gemm_kernel<FewBf16, 4>), grid, block, 0, st, g);
+        }
     };
-    auto gemm = [&](const FewSide& r, const FewSide& s) {
-        FewGemmArgs g{r, s, idx, S, K, p.r_experts * r.slabs * r.splits};
-        const dim3 grid((unsigned)(g.r_items + s.slabs * s.splits));
-        if (i8) hipLaunchKernelGGL(few_gemm_kernel<FewI8>, grid, dim3(kFewThreads), 0, st, g);
-        else hipLaunchKernelGGL(few_gemm_kernel<FewBf16>, grid, dim3(kFewThreads), 0, st, g);
-    };
+    // A, W, out, row and column scales, rows of A, (set above), lda, a_div, Kd, N, groups
     const void* x = i8 ? (const void*)xq : (const void*)a->x;
-    gemm(side(x, S, K, a->W1, D, F, R, p.slabs1, p.split1, u),
-         side(x, S, 1, a->Ws1, D, Fs, S, p.slabs1s, p.split1, us));
-    const FewAct ar{u, h, hsc, a->s1, F, R, p.split1}, as{us, hs, hssc, a->ss1, Fs, Fs ? S : 0, p.split1};
-    const dim3 ga((unsigned)(ar.rows + as.rows));
-    if (i8) hipLaunchKernelGGL(few_act_kernel<true>, ga, dim3(kFewThreads), 0, st, ar, as, idx, xs, K);
-    else hipLaunchKernelGGL(few_act_kernel<false>, ga, dim3(kFewThreads), 0, st, ar, as, idx, xs, K);
-    gemm(side(h, R, 1, a->W2, F, D, R, p.slabs2, p.split2, y),
-         side(hs, S, 1, a->Ws2, Fs, D, S, Fs ? p.slabs2 : 0, p.split2s, ys));
-    const FewOut orr{y, hsc, a->s2, R, p.split2}, os{ys, hssc, a->ss2, Fs ? S : 0, p.split2s};
-    const dim3 gc((unsigned)cdiv(D, 256), (unsigned)S);
-    if (i8) hipLaunchKernelGGL(few_combine_kernel<true>, gc, dim3(64), 0, st, orr, os, idx, prob, K, D, a->y);
-    else hipLaunchKernelGGL(few_combine_kernel<false>, gc, dim3(64), 0, st, orr, os, idx, prob, K, D, a->y);
+    gemm(FewSide{x, a->W1, h, xs, a->s1, S, 0, 0, K, D, F, 0}, FewSide{x, a->Ws1, hs, xs, a->ss1, S, 0, 0, 1, D, Fs, 0},
+         p.wk1, true);
+    const void *hr = h, *hsr = hs;
+    if (i8) {
+        const FewRows qr{h, hq, sc, F, R}, qs{hs, hqs, scs, Fs, Fs ? S : 0};
+        hipLaunchKernelGGL(few_quant_kernel, dim3((unsigned)(qr.rows + qs.rows)), dim3(kFewThreads), 0, st, qr, qs);
+        hr = hq;
+        hsr = hqs;
+    }
+    gemm(FewSide{hr, a->W2, y, sc, a->s2, R, 0, 0, 1, F, D, 0}, FewSide{hsr, a->Ws2, ys, scs, a->ss2, S, 0, 0, 1, Fs, D, 0},
+         p.wk2, false);
+    hipLaunchKernelGGL(few_combine_kernel, dim3((unsigned)cdiv(D, 256), (unsigned)S), dim3(kFewThreads), 0, st, y,
+                       Fs ? ys : nullptr, prob, K, D, a->y);
     return launch_check(st);
 }
 

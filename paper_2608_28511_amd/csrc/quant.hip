@@ -8,17 +8,18 @@
 
 namespace moe {
 
-// One row per wave (WAVES = 1, four rows a workgroup) or per workgroup (WAVES =
-// 16): the row is read once, 16 bytes a lane, and stays in registers between its
-// maximum and its codes.  With sched.tiles set, the last workgroup builds the grouped
-// GEMM's tile tables instead.
-constexpr int kQuantChunks = 8;   // 16-byte chunks a lane holds: 4,096 elements a wave, 65,536 a workgroup of 16
-template <int WAVES>
+// ROWS rows per wave (WAVES = 1, four waves a workgroup) or one per workgroup (WAVES =
+// 16): a row is read once, CH 16-byte chunks a lane, and stays in registers between its
+// maximum and its codes.  Eight chunks a lane are on their way before the first is used,
+// whatever the rows' length.  With sched.tiles set, the last workgroup builds the
+// grouped GEMM's tile tables instead.
+template <int WAVES, int ROWS, int CH>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void quant_rows_kernel(
     const uint16_t* __restrict__ x, int64_t R, int D, int8_t* __restrict__ q, float* __restrict__ scale,
     const int32_t* __restrict__ offsets, int E, SchedPart small, SchedPart large) {
+    static_assert(WAVES == 1 || ROWS == 1, "a workgroup of many waves takes one row");
     __shared__ uint32_t tops[WAVES];
-    constexpr int kRowsPerWg = WAVES == 1 ? 4 : 1;
+    constexpr int kRowsPerWg = WAVES == 1 ? 4 * ROWS : 1;
     if (small.tiles != nullptr && blockIdx.x == gridDim.x - 1) {
         build_tile_schedule(offsets, E, (int)R, small, large);
         return;
@@ -27,34 +28,40 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void quant_rows_kern
     const int64_t step = (int64_t)(gridDim.x - (small.tiles != nullptr ? 1 : 0)) * kRowsPerWg;
     const int first = WAVES == 1 ? lane : (int)threadIdx.x;
     const int n = D / 8;
-    for (int64_t r = (int64_t)blockIdx.x * kRowsPerWg + (WAVES == 1 ? wave : 0); r < R; r += step) {
-        const uint4* src = (const uint4*)(x + r * D);
-        uint4 v[kQuantChunks];
-        uint32_t top = 0;
+    for (int64_t r0 = (int64_t)blockIdx.x * kRowsPerWg + (WAVES == 1 ? wave * ROWS : 0); r0 < R; r0 += step) {
+        uint4 v[ROWS][CH];
 #pragma unroll
-        for (int i = 0; i < kQuantChunks; ++i) {
-            const int c = first + i * WAVES * 64;
-            v[i] = c < n ? ld_nt(src + c) : make_uint4(0u, 0u, 0u, 0u);
-        }
+        for (int j = 0; j < ROWS; ++j)
 #pragma unroll
-        for (int i = 0; i < kQuantChunks; ++i)
-            top = max_mag(max_mag(max_mag(max_mag(top, v[i].x), v[i].y), v[i].z), v[i].w);
-        top = wave_max_u32(top);
-        if constexpr (WAVES > 1) {
-            __syncthreads();   // the last row's maxima are read
-            if (lane == 0) tops[wave] = top;
-            __syncthreads();
+            for (int i = 0; i < CH; ++i) {
+                const int c = first + i * WAVES * 64;
+                v[j][i] = c < n && r0 + j < R ? ld_nt((const uint4*)(x + (r0 + j) * D) + c) : make_uint4(0u, 0u, 0u, 0u);
+            }
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) top = max(top, tops[w]);
-        }
-        Quant8 s;
-        s.init(top);
-        if (first == 0) scale[r] = s.scale;
-        uint2* dst = (uint2*)(q + r * D);
+        for (int j = 0; j < ROWS; ++j) {
+            const int64_t r = r0 + j;
+            if (r >= R) break;
+            uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < kQuantChunks; ++i) {
-            const int c = first + i * WAVES * 64;
-            if (c < n) dst[c] = make_uint2(codes4(s, v[i].x, v[i].y), codes4(s, v[i].z, v[i].w));
+            for (int i = 0; i < CH; ++i)
+                top = max_mag(max_mag(max_mag(max_mag(top, v[j][i].x), v[j][i].y), v[j][i].z), v[j][i].w);
+            top = wave_max_u32(top);
+            if constexpr (WAVES > 1) {
+                __syncthreads();   // the last row's maxima are read
+                if (lane == 0) tops[wave] = top;
+                __syncthreads();
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) top = max(top, tops[w]);
+            }
+            Quant8 s;
+            s.init(top);
+            if (first == 0) scale[r] = s.scale;
+            uint2* dst = (uint2*)(q + r * D);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const int c = first + i * WAVES * 64;
+                if (c < n) dst[c] = make_uint2(codes4(s, v[j][i].x, v[j][i].y), codes4(s, v[j][i].z, v[j][i].w));
+            }
         }
     }
 }
@@ -69,14 +76,19 @@ hipError_t launch_quant_rows(const moe_bf16* x, int64_t R, int D, int8_t* q, flo
         sl = sched_part(sched, E, R, true);
         extra = 1;
     }
-    // one row a wave or workgroup until the launch has 2^20 workgroups, then in turns
-    const int64_t most = 1 << 20;
-    if (D <= 64 * 8 * kQuantChunks)
-        hipLaunchKernelGGL(quant_rows_kernel<1>, dim3((unsigned)std::min((R + 3) / 4, most) + extra), dim3(256), 0, st, x, R, D, q, scale,
-                           sched_offsets, E, ss, sl);
-    else
-        hipLaunchKernelGGL(quant_rows_kernel<16>, dim3((unsigned)std::min(R, most) + extra), dim3(1024), 0, st, x, R, D, q, scale,
-                           sched_offsets, E, ss, sl);
+    auto go = [&](auto kernel, int rows, int threads) {   // in turns past 2^20 workgroups
+        const int64_t need = (R + rows - 1) / rows;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(need, (int64_t)1 << 20) + extra), dim3(threads), 0, st, x, R, D,
+                           q, scale, sched_offsets, E, ss, sl);
+    };
+    // Several rows a wave only where every CU has waves enough without them.
+    const bool many = R >= 64 * (int64_t)cu_count();
+    if (D <= 512 && many) go(quant_rows_kernel<1, 8, 1>, 32, 256);
+    else if (D <= 1024 && many) go(quant_rows_kernel<1, 4, 2>, 16, 256);
+    else if (D <= 2048) many ? go(quant_rows_kernel<1, 2, 4>, 8, 256) : go(quant_rows_kernel<1, 1, 4>, 4, 256);
+    else if (D <= 4096) go(quant_rows_kernel<1, 1, 8>, 4, 256);
+    else if (D <= 8192) go(quant_rows_kernel<1, 1, 16>, 4, 256);
+    else go(quant_rows_kernel<16, 1, 8>, 1, 1024);
     return launch_check(st);
 }
 
@@ -125,8 +137,9 @@ __global__ __launch_bounds__(256) void quant_weights_kernel(const uint16_t* __re
             const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                tile[c + 2 * u][kr + 32 * h] = (int8_t)s[2 * u].code(bf16_lo(w[u]));
-                tile[c + 2 * u + 1][kr + 32 * h] = (int8_t)s[2 * u + 1].code(bf16_hi(w[u]));
+                tile[c + 2 * u][kr + 32 * h] = s[2 * u].zero() ? 0 : (int8_t)s[2 * u].code(bf16_lo(w[u]));
+                tile[c + 2 * u + 1][kr + 32 * h] =
+                    s[2 * u + 1].zero() ? 0 : (int8_t)s[2 * u + 1].code(bf16_hi(w[u]));
             }
         }
         __syncthreads();
