@@ -934,6 +934,7 @@ int moe_latent_proj_i8(const moe_bf16* A, const int8_t* Wq, const float* w_scale
     MOE_TRY(need(C, (uint64_t)M * N * 2, 16));
     if (ws == nullptr || ws_bytes < moe_latent_proj_i8_workspace_bytes(M, Kd)) return MOE_ERR_WORKSPACE;
     MOE_TRY(opt(ws, 256));
+    if (moe::proj_few_fits(M, Kd)) return hip_status(moe::launch_proj_few(A, Wq, w_scale, M, N, Kd, C, stream));
     int8_t* q = (int8_t*)ws;
     float* scale = (float*)((char*)ws + align256((size_t)M * Kd));
     MOE_HIP(moe::launch_quant_rows(A, M, Kd, q, scale, stream));

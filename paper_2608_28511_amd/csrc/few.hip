@@ -13,26 +13,17 @@
 //   few_gemm     down: y_k = h W2 in fp32
 //   few_combine  y = bf16(sum_k p_k y_k + shared), all sums in fp32 and fixed order
 //
-// few_gemm's matrix products take 16 tokens; weights go from memory to the matrix
-// cores' operands in registers, several steps ahead, and never through LDS: every
-// weight is used by one wave only.  The waves of a workgroup share a slab of output
-// columns, each a part of its contraction.
 #include <algorithm>
 
 #include "kernels.h"
 #include "quant8.h"
 #include "score.h"
-#include "tile_dma.h"
+#include "thin.h"
 
 namespace moe {
 
-constexpr uint32_t kFewDrop = 0x80000000u;   // beyond any descriptor's range: reads as zero
-constexpr int kFewThreads = 256;
-typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t few_rsrc(const void* base, int64_t bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int32_t)bytes, 0x00020000);
-}
+constexpr int kFewThreads = kThinThreads;
+static_assert(kFewMaxTokens <= kThinRows, "an expert's rows are at most the tokens");
 
 // ---- router ---------------------------------------------------------------
 // part[chunk][t][e] = sum over 64 d of x[t, d] Wr[d, e].  A lane is an expert and a
@@ -84,42 +75,126 @@ __device__ __forceinline__ uint32_t wave_max_code(uint32_t v) {
     return max(max(a, b), max(c, d));
 }
 
-// Workgroup t < S: token t's logits, its K best experts and their weights.  Its first
-// wave picks: lane l holds experts l EPL .. + EPL - 1, so the lowest lane with the largest
-// code holds the lowest expert.  Workgroup S + t (8-bit weights): token t's codes.
+// The K largest codes of a wave, in order, ties to the lower expert: pick k goes to lane k.
+// Lane l holds experts l EPL .. + EPL - 1 and top, the largest of their codes.  The K-th
+// largest of the lanes' tops bounds the K-th largest code from below, so only codes from
+// there on can be picked (at least K of them, since at least K lanes hold an expert: EPL
+// is the least power of two with 64 EPL >= E, and K <= 32).  They are gathered in LDS, one
+// a lane, and each counts those before it: no chain of K rounds (3 tokens, 512 experts
+// top-22: 10.0 -> 6.5 us, the sums of the logits included).
+template <int EPL>
+__device__ __forceinline__ void few_pick(const uint32_t (&code)[EPL], uint32_t top, int K, uint32_t* codes, uint2* cand,
+                                         int& my_e, uint32_t& my_c) {
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+#pragma unroll 16
+    for (int j = 0; j < 64; ++j) {
+        const uint32_t o = __builtin_amdgcn_readlane(top, j);
+        before += o > top || (o == top && j < lane) ? 1 : 0;
+    }
+    if constexpr (EPL == 1) {   // the lanes' ranks themselves
+        if (before < K) cand[before] = make_uint2(top, (uint32_t)lane);
+        if (lane < K) {
+            const uint2 mine = cand[lane];
+            my_c = mine.x;
+            my_e = (int)mine.y;
+        }
+        return;
+    }
+    const uint32_t bound = __builtin_amdgcn_readlane(top, __builtin_ctzll(__ballot(before == K - 1)));
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+        const bool in = code[i] >= bound && code[i] != 0u;
+        const uint64_t m = __ballot(in);
+        const int at = n + __popcll(m & ((1ull << lane) - 1ull));
+        if (in && at < 64) cand[at] = make_uint2(code[i], (uint32_t)(lane * EPL + i));
+        n += __popcll(m);
+    }
+    if (n > 64) {   // many equal scores: K rounds of the wave's maximum, its lowest holder, and clearing it
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) codes[lane * EPL + i] = code[i];
+        for (int k = 0; k < K; ++k) {   // K <= E: the maximum is never a cleared code
+            uint32_t t = 0u;
+            int at = 0;
+            for (int i = EPL - 1; i >= 0; --i) {
+                const uint32_t c = codes[lane * EPL + i];
+                at = c >= t ? i : at;
+                t = max(t, c);
+            }
+            const uint32_t m = wave_max_code(t);
+            const int owner = __builtin_ctzll(__ballot(t == m));
+            if (lane == owner) codes[lane * EPL + at] = 0u;
+            const int e = __builtin_amdgcn_readlane(lane * EPL + at, owner);
+            if (lane == k) {
+                my_e = e;
+                my_c = m;
+            }
+        }
+        return;
+    }
+    // larger code first, then the lower expert; the lanes of one wave write and read cand in order
+    const uint2 c = lane < n ? cand[lane] : make_uint2(0u, 1023u);
+    int rank = 0;
+    for (int j = 0; j < n; ++j) {
+        const uint32_t oc = __builtin_amdgcn_readlane(c.x, j), oe = __builtin_amdgcn_readlane(c.y, j);
+        rank += oc > c.x || (oc == c.x && oe < c.y) ? 1 : 0;
+    }
+    if (lane < n && rank < K) cand[rank] = c;
+    if (lane < K) {
+        const uint2 mine = cand[lane];
+        my_c = mine.x;
+        my_e = (int)mine.y;
+    }
+}
+
+// Workgroup t < S: token t's logits, its K best experts (picked by its first wave) and
+// their weights.  Workgroup S + t (8-bit weights): token t's codes.
+constexpr int kRouteThreads = 1024;
 template <int EPL, bool SIG>
-__global__ __launch_bounds__(kFewThreads) void few_route_kernel(
+__global__ __launch_bounds__(kRouteThreads) void few_route_kernel(
     const float* __restrict__ part, int nd, const float* __restrict__ bias, const float* __restrict__ sel_bias, int S,
     int E, int K, int32_t* __restrict__ topk_idx, float* __restrict__ topk_prob, const uint16_t* __restrict__ x, int D,
     int8_t* __restrict__ xq, float* __restrict__ xs) {
     __shared__ float lg[1024];
-    __shared__ uint32_t tops[4];
+    __shared__ uint32_t tops[kRouteThreads / 64];
+    __shared__ uint32_t codes[64 * EPL];
+    __shared__ uint2 cand[64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     if ((int)blockIdx.x >= S) {
         const int t = blockIdx.x - S;
         const uint4* src = (const uint4*)(x + (int64_t)t * D);
         uint32_t top = 0;
-        for (int c = tid; c < D / 8; c += kFewThreads) {
+        for (int c = tid; c < D / 8; c += kRouteThreads) {
             const uint4 v = src[c];
             top = max_mag(max_mag(max_mag(max_mag(top, v.x), v.y), v.z), v.w);
         }
         top = wave_max_u32(top);
         if (lane == 0) tops[wave] = top;
         __syncthreads();
+        for (int w = 0; w < kRouteThreads / 64; ++w) top = max(top, tops[w]);
         Quant8 s;
-        s.init(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
+        s.init(top);
         if (tid == 0) xs[t] = s.scale;
-        for (int c = tid; c < D / 8; c += kFewThreads) {
+        for (int c = tid; c < D / 8; c += kRouteThreads) {
             const uint4 v = src[c];
             ((uint2*)(xq + (int64_t)t * D))[c] = make_uint2(codes4(s, v.x, v.y), codes4(s, v.z, v.w));
         }
         return;
     }
+    // 64 EPL experts side by side, the chunks of d dealt to the threads that are left
     const int t = blockIdx.x;
-    for (int e = tid; e < E; e += kFewThreads) {
-        float a = 0.f;
+    constexpr int kSide = 64 * EPL, kParts = kRouteThreads / kSide;
+    const int e = tid % kSide, p = tid / kSide;
+    float a = 0.f;
+    if (e < E) {
 #pragma unroll 8
-        for (int c = 0; c < nd; ++c) a += part[((int64_t)c * S + t) * E + e];
+        for (int c = p; c < nd; c += kParts) a += part[((int64_t)c * S + t) * E + e];
+    }
+    lg[tid] = a;
+    __syncthreads();
+    if (p == 0 && e < E) {
+        for (int q = 1; q < kParts; ++q) a += lg[q * kSide + e];
         lg[e] = bias != nullptr ? a + bias[e] : a;
     }
     __syncthreads();
@@ -139,26 +214,7 @@ __global__ __launch_bounds__(kFewThreads) void few_route_kernel(
     }
     int my_e = 0;
     uint32_t my_c = 0u;
-    for (int k = 0; k < K; ++k) {   // K <= E: the maximum is never a cleared code
-        const uint32_t m = wave_max_code(top);
-        const int owner = __builtin_ctzll(__ballot(top == m));
-        int i_sel = 0;
-#pragma unroll
-        for (int i = EPL - 1; i >= 0; --i) i_sel = code[i] == m ? i : i_sel;
-        const int e = __builtin_amdgcn_readlane(lane * EPL + i_sel, owner);
-        if (lane == owner) {
-            top = 0u;
-#pragma unroll
-            for (int i = 0; i < EPL; ++i) {
-                code[i] = i == i_sel ? 0u : code[i];
-                top = max(top, code[i]);
-            }
-        }
-        if (lane == k) {
-            my_e = e;
-            my_c = m;
-        }
-    }
+    few_pick<EPL>(code, top, K, codes, cand, my_e, my_c);
     float z = 0.f;
     if constexpr (SIG) {
         if (lane < K) z = sigmoid_f32(lg[my_e]);
@@ -186,30 +242,41 @@ struct FewSide {
     int64_t a_bytes, w_bytes;   // of A, of one expert's W
     int lda, a_div;
     int Kd, N;
-    int groups;          // workgroups an expert takes
+    int groups;          // workgroups an expert takes (0: there is no such expert)
 };
 struct FewGemmArgs {
     FewSide routed, shared;
     const int32_t* idx;   // [S, K]
     int S, K, r_items;    // workgroups of the routed experts
     int wk;               // waves that share a slab's contraction; 4 / wk slabs side by side in a workgroup
-    int up;
+    int epi;
 };
 
 // The a-th expert (ascending) among the n picks and its rows, in order, in rows[];
-// returns the expert, or -1 if fewer are picked.  Every thread of the workgroup calls it.
-__device__ __forceinline__ int few_plan(const int32_t* __restrict__ idx, int n, int a, uint32_t* seen, int32_t* picks,
-                                        int32_t* rows, int32_t* nrows) {
-    const int tid = threadIdx.x, lane = tid & 63;
-    if (tid < 32) seen[tid] = 0u;
+// returns the expert, or -1 if fewer are picked.  A single token's picks are distinct and
+// need no order.  Every thread of the workgroup calls it.
+struct FewPicks {
+    uint32_t seen[32];
+    int32_t picks[kFewMaxTokens * 32], rows[kFewMaxTokens], nrows;
+};
+__device__ __forceinline__ int few_plan(const int32_t* __restrict__ idx, int S, int K, int a, FewPicks& sh) {
+    const int tid = threadIdx.x, lane = tid & 63, n = S * K;
+    if (S == 1) {
+        if (tid == 0) {
+            sh.rows[0] = a;
+            sh.nrows = 1;
+        }
+        return a < K ? __builtin_amdgcn_readfirstlane(idx[a]) & 1023 : -1;
+    }
+    if (tid < 32) sh.seen[tid] = 0u;
     __syncthreads();
     for (int q = tid; q < n; q += kFewThreads) {
         const int e = idx[q] & 1023;   // E <= 1024
-        picks[q] = e;
-        atomicOr(&seen[e >> 5], 1u << (e & 31));
+        sh.picks[q] = e;
+        atomicOr(&sh.seen[e >> 5], 1u << (e & 31));
     }
     __syncthreads();
-    const uint32_t word = lane < 32 ? seen[lane] : 0u;
+    const uint32_t word = lane < 32 ? sh.seen[lane] : 0u;
     int incl = __popc(word);
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -226,213 +293,21 @@ __device__ __forceinline__ int few_plan(const int32_t* __restrict__ idx, int n, 
     if (tid < 64) {
         int at = 0;
         for (int q0 = 0; q0 < n; q0 += 64) {
-            const bool hit = q0 + lane < n && picks[q0 + lane] == e;
+            const bool hit = q0 + lane < n && sh.picks[q0 + lane] == e;
             const uint64_t m = __ballot(hit);
             const int pos = at + __popcll(m & ((1ull << lane) - 1ull));
-            if (hit && pos < kFewMaxTokens) rows[pos] = q0 + lane;   // a token picks an expert once
+            if (hit && pos < kFewMaxTokens) sh.rows[pos] = q0 + lane;   // a token picks an expert once
             at += __popcll(m);
         }
-        if (lane == 0) *nrows = at < kFewMaxTokens ? at : kFewMaxTokens;
+        if (lane == 0) sh.nrows = at < kFewMaxTokens ? at : kFewMaxTokens;
     }
     return e;
-}
-
-// bf16 weights, N-contiguous: slabs of 64 columns, steps of 32 k.  A lane loads 4
-// columns of 8 k rows (each load of the wave four whole cache lines) and packs them into
-// the fragments of columns 4 c + q, q = 0 .. 3, with one byte permutation a register.
-struct FewBf16 {
-    static constexpr bool kI8 = false;
-    static constexpr int kCols = 64, kStep = 32, kAcc = 4;
-    template <int MB>
-    static constexpr int kAhead = MB == 4 ? 3 : 4;
-    u32x2 w[8];
-
-    __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t& rw, const FewSide& s, int n0, int k, int lane) {
-        const int g = lane >> 4, c = lane & 15;
-        const uint32_t ld = (uint32_t)s.N * 2;
-        const uint32_t o = n0 + 4 * c < s.N ? (uint32_t)(k + 8 * g) * ld + (uint32_t)(n0 + 4 * c) * 2 : kFewDrop;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = __builtin_amdgcn_raw_buffer_load_b64(rw, o + (uint32_t)j * ld, 0, 0);
-    }
-    template <int MB>
-    struct A {
-        u32x4 v[MB];
-        __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t& ra, const uint32_t (&row)[MB], int k, int Kd,
-                                             int lane) {
-            const int kk = k + 8 * (lane >> 4);
-#pragma unroll
-            for (int m = 0; m < MB; ++m)
-                v[m] = __builtin_amdgcn_raw_buffer_load_b128(ra, kk < Kd ? row[m] + (uint32_t)kk * 2 : kFewDrop, 0, 0);
-        }
-    };
-    template <int MB>
-    __device__ __forceinline__ void mma(f32x4 (&acc)[MB][kAcc], const A<MB>& a) const {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            u32x4 f;
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                f[u] = __builtin_amdgcn_perm(w[2 * u + 1][q >> 1], w[2 * u][q >> 1], q & 1 ? 0x07060302u : 0x05040100u);
-#pragma unroll
-            for (int m = 0; m < MB; ++m)
-                acc[m][q] = mfma16<false>(__builtin_bit_cast(bf16x8, f), __builtin_bit_cast(bf16x8, a.v[m]), acc[m][q]);
-        }
-    }
-    // acc[q][v] of a lane is column 16 g + 4 v + q of its token: piece v is four columns
-    __device__ __forceinline__ static f32x4 piece(const f32x4 (&acc)[kAcc], int v) {
-        return f32x4{acc[0][v], acc[1][v], acc[2][v], acc[3][v]};
-    }
-    __device__ __forceinline__ static int piece_col(int v, int lane) { return 16 * (lane >> 4) + 4 * v; }
-};
-
-// 8-bit weights, K-contiguous: slabs of 32 columns, steps of 128 k, whose fragments
-// are 16 bytes of a channel as they lie in memory.
-struct FewI8 {
-    static constexpr bool kI8 = true;
-    static constexpr int kCols = 32, kStep = 128, kAcc = 2;
-    template <int MB>
-    static constexpr int kAhead = MB == 4 ? 2 : 3;
-    u32x4 w[2][2];
-
-    __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t& rw, const FewSide& s, int n0, int k, int lane) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const int n = n0 + 16 * b + (lane & 15);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int kk = k + 64 * h + 16 * (lane >> 4);
-                const uint32_t o = n < s.N && kk < s.Kd ? (uint32_t)n * (uint32_t)s.Kd + (uint32_t)kk : kFewDrop;
-                w[b][h] = __builtin_amdgcn_raw_buffer_load_b128(rw, o, 0, 0);
-            }
-        }
-    }
-    template <int MB>
-    struct A {
-        u32x4 v[MB][2];
-        __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t& ra, const uint32_t (&row)[MB], int k, int Kd,
-                                             int lane) {
-#pragma unroll
-            for (int m = 0; m < MB; ++m)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int kk = k + 64 * h + 16 * (lane >> 4);
-                    v[m][h] = __builtin_amdgcn_raw_buffer_load_b128(ra, kk < Kd ? row[m] + (uint32_t)kk : kFewDrop, 0, 0);
-                }
-        }
-    };
-    template <int MB>
-    __device__ __forceinline__ void mma(f32x4 (&acc)[MB][kAcc], const A<MB>& a) const {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int m = 0; m < MB; ++m)
-                    acc[m][b] = mfma16<true>(__builtin_bit_cast(bf16x8, w[b][h]), __builtin_bit_cast(bf16x8, a.v[m][h]),
-                                             acc[m][b]);
-    }
-    __device__ __forceinline__ static f32x4 piece(const f32x4 (&acc)[kAcc], int b) { return acc[b]; }
-    __device__ __forceinline__ static int piece_col(int b, int lane) { return 16 * b + 4 * (lane >> 4); }
-};
-
-template <bool I8>
-__device__ __forceinline__ f32x4 few_add(f32x4 a, f32x4 b) {
-    if constexpr (I8)
-        return __builtin_bit_cast(f32x4, __builtin_bit_cast(i32x4, a) + __builtin_bit_cast(i32x4, b));
-    else
-        return a + b;
-}
-
-// Columns [n0, n0 + kCols) of the product for 16 MB rows of expert e.  The wave is the
-// kk-th of the wk that share the slab: it takes every wk-th step, and their sums are
-// joined through LDS in wave order, each wave finishing some of the slab's pieces.
-// Every wave of the workgroup calls it (n0 may lie past N: such a slab has nothing to do).
-template <class T, int MB>
-__device__ __forceinline__ void few_body(const FewGemmArgs& p, const FewSide& s, int e, int n0, int kk, int wk,
-                                         const int32_t* rows, int nrows, f32x4 (*red)[T::kAcc][64]) {
-    constexpr int P = T::template kAhead<MB>;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int nst = (s.Kd + T::kStep - 1) / T::kStep;
-    const int mine = n0 < s.N && nst > kk ? (nst - kk + wk - 1) / wk : 0;
-    const __amdgpu_buffer_rsrc_t rw = few_rsrc((const char*)s.W + e * s.w_bytes, s.w_bytes);
-    const __amdgpu_buffer_rsrc_t ra = few_rsrc(s.A, s.a_bytes);
-    uint32_t row[MB];
-#pragma unroll
-    for (int m = 0; m < MB; ++m) {
-        const int i = m * 16 + (lane & 15);
-        row[m] = i < nrows ? (uint32_t)(rows[i] / s.a_div) * (uint32_t)s.lda : kFewDrop;
-    }
-    f32x4 acc[MB][T::kAcc];
-#pragma unroll
-    for (int m = 0; m < MB; ++m)
-#pragma unroll
-        for (int q = 0; q < T::kAcc; ++q) acc[m][q] = f32x4{0.f, 0.f, 0.f, 0.f};
-    T w[P];
-    typename T::template A<MB> a[P];
-    auto load = [&](int slot, int i) {
-        const int k = (kk + wk * i) * T::kStep;
-        w[slot].load(rw, s, n0, k, lane);
-        a[slot].load(ra, row, k, s.Kd, lane);
-    };
-#pragma unroll
-    for (int q = 0; q < P; ++q)
-        if (q < mine) load(q, q);
-    for (int i0 = 0; i0 < mine; i0 += P) {
-#pragma unroll
-        for (int q = 0; q < P; ++q) {
-            if (i0 + q >= mine) break;
-            w[q].template mma<MB>(acc, a[q]);
-            if (i0 + q + P < mine) load(q, i0 + q + P);
-        }
-    }
-    auto leave = [&](int m, int v, f32x4 t) {
-        const int i = m * 16 + (lane & 15), col = n0 + T::piece_col(v, lane);
-        if (i >= nrows || col >= s.N) return;   // N is a multiple of 8
-        const int r = rows[i];
-        if constexpr (T::kI8) {
-            const float rs = s.row_scale[r / s.a_div];
-            const f32x4 cs = *(const f32x4*)(s.col_scale + (int64_t)e * s.N + col);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) t[q] = (float)__float_as_int(t[q]) * rs * cs[q];
-        }
-        const int64_t at = (int64_t)r * s.N + col;
-        if (p.up) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                t[q] = relu_f32(t[q]);
-                t[q] *= t[q];
-            }
-            *(u32x2*)((uint16_t*)s.out + at) = u32x2{pack_bf16x2(t[0], t[1]), pack_bf16x2(t[2], t[3])};
-        } else {
-            *(f32x4*)((float*)s.out + at) = t;
-        }
-    };
-#pragma unroll
-    for (int m = 0; m < MB; ++m) {
-        if (m > 0 && m * 16 >= nrows) break;
-        if (wk == 1) {
-#pragma unroll
-            for (int v = 0; v < T::kAcc; ++v) leave(m, v, T::piece(acc[m], v));
-        } else {
-            if (m > 0) __syncthreads();
-#pragma unroll
-            for (int v = 0; v < T::kAcc; ++v) red[wave][v][lane] = T::piece(acc[m], v);
-            __syncthreads();
-            const int first = wave - kk;
-            for (int v = kk; v < T::kAcc; v += wk) {
-                f32x4 t = red[first][v][lane];
-                for (int j = 1; j < wk; ++j) t = few_add<T::kI8>(t, red[first + j][v][lane]);
-                leave(m, v, t);
-            }
-        }
-    }
 }
 
 // MBMAX = 1: at most 16 tokens, so at most 16 rows an expert; four waves a SIMD.
 template <class T, int MBMAX>
 __global__ __launch_bounds__(kFewThreads, MBMAX == 1 ? 4 : 2) void few_gemm_kernel(FewGemmArgs p) {
-    __shared__ uint32_t seen[32];
-    __shared__ int32_t picks[(MBMAX == 1 ? 16 : kFewMaxTokens) * 32], rows[kFewMaxTokens], nrows_s;
+    __shared__ FewPicks sh;
     __shared__ f32x4 red[4][T::kAcc][64];   // wk > 1: every wave's sums
     const bool shared = (int)blockIdx.x >= p.r_items;
     const int b = (int)blockIdx.x - (shared ? p.r_items : 0);
@@ -440,20 +315,20 @@ __global__ __launch_bounds__(kFewThreads, MBMAX == 1 ? 4 : 2) void few_gemm_kern
     const int a = b / s.groups, in = b - a * s.groups;
     int e = 0;
     if (shared) {
-        if ((int)threadIdx.x < p.S) rows[threadIdx.x] = threadIdx.x;
-        if (threadIdx.x == 0) nrows_s = p.S;
+        if ((int)threadIdx.x < p.S) sh.rows[threadIdx.x] = threadIdx.x;
+        if (threadIdx.x == 0) sh.nrows = p.S;
     } else {
-        e = few_plan(p.idx, p.S * p.K, a, seen, picks, rows, &nrows_s);
+        e = few_plan(p.idx, p.S, p.K, a, sh);
         if (e < 0) return;
     }
     __syncthreads();
-    const int nrows = __builtin_amdgcn_readfirstlane(nrows_s);
+    const int nrows = __builtin_amdgcn_readfirstlane(sh.nrows);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wk = p.wk;
-    const int kk = wave & (wk - 1), wn = wave / wk;
-    const int n0 = (in * (4 / wk) + wn) * T::kCols;
-    if (MBMAX == 1 || nrows <= 16) few_body<T, 1>(p, s, e, n0, kk, wk, rows, nrows, red);
-    else if (nrows <= 32) few_body<T, MBMAX == 1 ? 1 : 2>(p, s, e, n0, kk, wk, rows, nrows, red);
-    else few_body<T, MBMAX == 1 ? 1 : 4>(p, s, e, n0, kk, wk, rows, nrows, red);
+    const int kk = wave & (wk - 1), n0 = (in * (4 / wk) + wave / wk) * T::kCols;
+    const ThinArgs t{s.A, (const char*)s.W + e * s.w_bytes, s.out, s.row_scale, s.col_scale + (int64_t)e * s.N,
+                     s.a_bytes, s.w_bytes, s.lda, s.Kd, s.N, p.epi};
+    thin_rows<T, MBMAX>(t, n0, kk, wk, nrows, [&](int i) { return sh.rows[i] / s.a_div; },
+                        [&](int i) { return sh.rows[i]; }, red);
 }
 
 // ---- between the products and after them ------------------------------------
@@ -533,7 +408,7 @@ __global__ __launch_bounds__(kFewThreads) void few_combine_kernel(const float* _
     __syncthreads();
     if (wave != 0 || d >= D) return;
     v = ((sum[0][lane] + sum[1][lane]) + sum[2][lane]) + sum[3][lane];
-    *(u32x2*)(y + (int64_t)t * D + d) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    *(u32x2_thin*)(y + (int64_t)t * D + d) = u32x2_thin{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
 }
 
 // ---- host -------------------------------------------------------------------
@@ -559,12 +434,20 @@ int few_share(int picks, int steps) {
     return std::min(most, steps >= 4 ? 4 : steps >= 2 ? 2 : 1);
 }
 
+// Columns of a slab.  8-bit weights take 32, or with more than 16 tokens 64, which halves
+// how often the workgroups read the rows (64 tokens of 64 experts 86 -> 78 us; 16 tokens
+// of 256: 186.4 with 32, 189.3 with 64).
+int few_cols(const moe_layer_few_args* a) {
+    if (a->weights != MOE_WEIGHTS_I8) return ThinBf16::kCols;
+    return a->S <= 16 ? ThinI8<2>::kCols : ThinI8<4>::kCols;
+}
+
 FewPlan few_plan_of(const moe_layer_few_args* a) {
     FewPlan p{};
     const int S = (int)a->S, D = a->D, E = a->E, K = a->K, F = a->F, Fs = a->Fs;
     const bool i8 = a->weights == MOE_WEIGHTS_I8;
     const size_t R = (size_t)S * K;
-    const int step = i8 ? FewI8::kStep : FewBf16::kStep;
+    const int step = i8 ? ThinI8<2>::kStep : ThinBf16::kStep;
     p.nd = cdiv(D, kFewD);
     p.r_experts = (int)std::min<size_t>((size_t)E, R);
     p.wk1 = few_share((int)R, cdiv(D, step));
@@ -596,10 +479,10 @@ template <int EPL>
 void launch_route_few(bool sig, dim3 g, hipStream_t st, const float* part, int nd, const moe_layer_few_args* a,
                       int32_t* idx, float* prob, int8_t* xq, float* xs) {
     if (sig)
-        hipLaunchKernelGGL((few_route_kernel<EPL, true>), g, dim3(kFewThreads), 0, st, part, nd, a->router_bias,
+        hipLaunchKernelGGL((few_route_kernel<EPL, true>), g, dim3(kRouteThreads), 0, st, part, nd, a->router_bias,
                            a->sel_bias, (int)a->S, a->E, a->K, idx, prob, a->x, a->D, xq, xs);
     else
-        hipLaunchKernelGGL((few_route_kernel<EPL, false>), g, dim3(kFewThreads), 0, st, part, nd, a->router_bias,
+        hipLaunchKernelGGL((few_route_kernel<EPL, false>), g, dim3(kRouteThreads), 0, st, part, nd, a->router_bias,
                            a->sel_bias, (int)a->S, a->E, a->K, idx, prob, a->x, a->D, xq, xs);
 }
 
@@ -611,7 +494,7 @@ hipError_t launch_layer_few(const moe_layer_few_args* a, hipStream_t st) {
     const FewPlan p = few_plan_of(a);
     const int S = (int)a->S, D = a->D, E = a->E, K = a->K, F = a->F, Fs = a->Fs, R = S * K;
     const bool i8 = a->weights == MOE_WEIGHTS_I8;
-    const int wb = i8 ? 1 : 2, cols = i8 ? FewI8::kCols : FewBf16::kCols;
+    const int wb = i8 ? 1 : 2, cols = few_cols(a);
     char* ws = (char*)a->ws;
     float* part = (float*)(ws + p.part);
     int32_t* idx = a->topk_idx != nullptr ? a->topk_idx : (int32_t*)(ws + p.idx);
@@ -631,27 +514,28 @@ hipError_t launch_layer_few(const moe_layer_few_args* a, hipStream_t st) {
     else if (E <= 512) launch_route_few<8>(sig, gr, st, part, p.nd, a, idx, prob, xq, xs);
     else launch_route_few<16>(sig, gr, st, part, p.nd, a, idx, prob, xq, xs);
 
-    auto gemm = [&](FewSide r, FewSide s, int wk, bool up) {
+    auto gemm = [&](FewSide r, FewSide s, int wk, int epi) {
         for (FewSide* q : {&r, &s}) {
             q->lda = q->Kd * wb;
             q->a_bytes *= q->lda;                       // given as rows
             q->w_bytes = (int64_t)q->Kd * q->N * wb;
             q->groups = cdiv(cdiv(q->N, cols), 4 / wk);
         }
-        const FewGemmArgs g{r, s, idx, S, K, p.r_experts * r.groups, wk, up ? 1 : 0};
-        const dim3 grid((unsigned)(g.r_items + (Fs ? s.groups : 0))), block(kFewThreads);
+        if (Fs == 0) s.groups = 0;
+        const FewGemmArgs g{r, s, idx, S, K, p.r_experts * r.groups, wk, epi};
+        const dim3 grid((unsigned)(g.r_items + s.groups)), block(kFewThreads);
         if (S <= 16) {
-            if (i8) hipLaunchKernelGGL((few_gemm_kernel<FewI8, 1>), grid, block, 0, st, g);
-            else hipLaunchKernelGGL((few_gemm_kernel<FewBf16, 1>), grid, block, 0, st, g);
+            if (i8) hipLaunchKernelGGL((few_gemm_kernel<ThinI8<2>, 1>), grid, block, 0, st, g);
+            else hipLaunchKernelGGL((few_gemm_kernel<ThinBf16, 1>), grid, block, 0, st, g);
         } else {
-            if (i8) hipLaunchKernelGGL((few_gemm_kernel<FewI8, 4>), grid, block, 0, st, g);
-            else hipLaunchKernelGGL((few_gemm_kernel<FewBf16, 4>), grid, block, 0, st, g);
+            if (i8) hipLaunchKernelGGL((few_gemm_kernel<ThinI8<4>, 4>), grid, block, 0, st, g);
+            else hipLaunchKernelGGL((few_gemm_kernel<ThinBf16, 4>), grid, block, 0, st, g);
         }
     };
-    // A, W, out, row and column scales, rows of A, (set above), lda, a_div, Kd, N, groups
+    // A, W, out, row and column scales, rows of A, .., .., a_div, Kd, N (the rest is set above)
     const void* x = i8 ? (const void*)xq : (const void*)a->x;
     gemm(FewSide{x, a->W1, h, xs, a->s1, S, 0, 0, K, D, F, 0}, FewSide{x, a->Ws1, hs, xs, a->ss1, S, 0, 0, 1, D, Fs, 0},
-         p.wk1, true);
+         p.wk1, THIN_RELU2);
     const void *hr = h, *hsr = hs;
     if (i8) {
         const FewRows qr{h, hq, sc, F, R}, qs{hs, hqs, scs, Fs, Fs ? S : 0};
@@ -659,8 +543,9 @@ hipError_t launch_layer_few(const moe_layer_few_args* a, hipStream_t st) {
         hr = hq;
         hsr = hqs;
     }
-    gemm(FewSide{hr, a->W2, y, sc, a->s2, R, 0, 0, 1, F, D, 0}, FewSide{hsr, a->Ws2, ys, scs, a->ss2, S, 0, 0, 1, Fs, D, 0},
-         p.wk2, false);
+    gemm(FewSide{hr, a->W2, y, sc, a->s2, R, 0, 0, 1, F, D, 0},
+         FewSide{hsr, a->Ws2, ys, scs, a->ss2, S, 0, 0, 1, Fs, D, 0},
+         p.wk2, THIN_F32);
     hipLaunchKernelGGL(few_combine_kernel, dim3((unsigned)cdiv(D, 256), (unsigned)S), dim3(kFewThreads), 0, st, y,
                        Fs ? ys : nullptr, prob, K, D, a->y);
     return launch_check(st);

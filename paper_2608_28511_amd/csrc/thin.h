@@ -1,0 +1,244 @@
+// Products of at most 64 rows with weights that are read once (internal to the
+// library): what bounds them is the reading, so weights go from memory to the matrix
+// cores' operands in registers, several steps ahead, and never through LDS, where the
+// wide tiles of gemm.hip keep theirs to use them again.  A slab of output columns belongs
+// to one wave, or to the two or four waves of a workgroup that share its contraction and join
+// their sums in LDS.
+#pragma once
+
+#include <type_traits>
+
+#include "common.h"
+#include "tile_dma.h"
+
+namespace moe {
+
+constexpr uint32_t kThinDrop = 0x80000000u;   // beyond any descriptor's range: reads as zero
+constexpr int kThinThreads = 256;
+constexpr int kThinRows = 64;
+typedef unsigned u32x2_thin __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t thin_rsrc(const void* base, int64_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int32_t)bytes, 0x00020000);
+}
+
+// What leaves a product: fp32, or bf16 of it, or bf16 of its squared ReLU.
+enum { THIN_F32 = 0, THIN_BF16 = 1, THIN_RELU2 = 2 };
+
+// One expert's product.
+struct ThinArgs {
+    const void* A;              // its rows start within a_bytes
+    const void* W;              // bf16 [Kd, N] or int8 [N, Kd]
+    void* out;                  // [rows][N]
+    const float* row_scale;     // 8-bit: by source row
+    const float* col_scale;     // 8-bit: [N]
+    int64_t a_bytes, w_bytes;
+    int lda;                    // bytes
+    int Kd, N;
+    int epi;
+};
+
+// bf16 weights, N-contiguous: slabs of 64 columns, steps of 32 k.  A lane loads 4
+// columns of 8 k rows (each load of the wave four whole cache lines) and packs them into
+// the fragments of columns 4 c + q, q = 0 .. 3, with one byte permutation a register.
+struct ThinBf16 {
+    static constexpr bool kI8 = false;
+    static constexpr int kCols = 64, kStep = 32, kAcc = 4;
+    template <int MB>
+    static constexpr int kAhead = MB == 4 ? 3 : 4;
+    u32x2_thin w[8];
+
+    __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t& rw, const ThinArgs& s, int n0, int k, int lane) {
+        const int g = lane >> 4, c = lane & 15;
+        const uint32_t ld = (uint32_t)s.N * 2;
+        const uint32_t o = n0 + 4 * c < s.N ? (uint32_t)(k + 8 * g) * ld + (uint32_t)(n0 + 4 * c) * 2 : kThinDrop;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = __builtin_amdgcn_raw_buffer_load_b64(rw, o + (uint32_t)j * ld, 0, 0);
+    }
+    template <int MB>
+    struct A {
+        u32x4 v[MB];
+        __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t& ra, const uint32_t (&row)[MB], int k, int Kd,
+                                             int lane) {
+            const int kk = k + 8 * (lane >> 4);
+#pragma unroll
+            for (int m = 0; m < MB; ++m)
+                v[m] = __builtin_amdgcn_raw_buffer_load_b128(ra, kk < Kd ? row[m] + (uint32_t)kk * 2 : kThinDrop, 0, 0);
+        }
+    };
+    template <int MB>
+    __device__ __forceinline__ void mma(f32x4 (&acc)[MB][kAcc], const A<MB>& a) const {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            u32x4 f;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                f[u] = __builtin_amdgcn_perm(w[2 * u + 1][q >> 1], w[2 * u][q >> 1], q & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+            for (int m = 0; m < MB; ++m)
+                acc[m][q] = mfma16<false>(__builtin_bit_cast(bf16x8, f), __builtin_bit_cast(bf16x8, a.v[m]), acc[m][q]);
+        }
+    }
+    // acc[q][v] of a lane is column 16 g + 4 v + q of its token: piece v is four columns
+    __device__ __forceinline__ static f32x4 piece(const f32x4 (&acc)[kAcc], int v) {
+        return f32x4{acc[0][v], acc[1][v], acc[2][v], acc[3][v]};
+    }
+    __device__ __forceinline__ static int piece_col(int v, int lane) { return 16 * (lane >> 4) + 4 * v; }
+};
+
+// 8-bit weights, K-contiguous: slabs of 16 NB columns, steps of 128 k, whose fragments
+// are 16 bytes of a channel as they lie in memory.
+template <int NB>
+struct ThinI8 {
+    static constexpr bool kI8 = true;
+    static constexpr int kCols = 16 * NB, kStep = 128, kAcc = NB;
+    template <int MB>
+    static constexpr int kAhead = MB == 4 || NB == 4 ? 2 : 3;
+    u32x4 w[NB][2];
+
+    __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t& rw, const ThinArgs& s, int n0, int k, int lane) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const int n = n0 + 16 * b + (lane & 15);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int kk = k + 64 * h + 16 * (lane >> 4);
+                const uint32_t o = n < s.N && kk < s.Kd ? (uint32_t)n * (uint32_t)s.Kd + (uint32_t)kk : kThinDrop;
+                w[b][h] = __builtin_amdgcn_raw_buffer_load_b128(rw, o, 0, 0);
+            }
+        }
+    }
+    template <int MB>
+    struct A {
+        u32x4 v[MB][2];
+        __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t& ra, const uint32_t (&row)[MB], int k, int Kd,
+                                             int lane) {
+#pragma unroll
+            for (int m = 0; m < MB; ++m)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int kk = k + 64 * h + 16 * (lane >> 4);
+                    v[m][h] = __builtin_amdgcn_raw_buffer_load_b128(ra, kk < Kd ? row[m] + (uint32_t)kk : kThinDrop, 0, 0);
+                }
+        }
+    };
+    template <int MB>
+    __device__ __forceinline__ void mma(f32x4 (&acc)[MB][kAcc], const A<MB>& a) const {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int m = 0; m < MB; ++m)
+                    acc[m][b] = mfma16<true>(__builtin_bit_cast(bf16x8, w[b][h]), __builtin_bit_cast(bf16x8, a.v[m][h]),
+                                             acc[m][b]);
+    }
+    __device__ __forceinline__ static f32x4 piece(const f32x4 (&acc)[kAcc], int b) { return acc[b]; }
+    __device__ __forceinline__ static int piece_col(int b, int lane) { return 16 * b + 4 * (lane >> 4); }
+};
+
+template <bool I8>
+__device__ __forceinline__ f32x4 thin_add(f32x4 a, f32x4 b) {
+    if constexpr (I8)
+        return __builtin_bit_cast(f32x4, __builtin_bit_cast(i32x4, a) + __builtin_bit_cast(i32x4, b));
+    else
+        return a + b;
+}
+
+// Columns [n0, n0 + kCols) of the product for 16 MB rows, of which nrows exist: src(i) is
+// row i's place in A and dst(i) its row in out.  The wave is the kk-th of the wk that share
+// the slab: it takes every wk-th step, and their sums are joined through LDS in wave
+// order, each wave finishing some of the slab's pieces.  Every wave of the workgroup calls
+// it (n0 may lie past N: such a slab has nothing to do).
+template <class T, int MB, class Src, class Dst>
+__device__ __forceinline__ void thin_body(const ThinArgs& s, int n0, int kk, int wk, int nrows, Src&& src, Dst&& dst,
+                                          f32x4 (*red)[T::kAcc][64]) {
+    constexpr int P = T::template kAhead<MB>;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int nst = (s.Kd + T::kStep - 1) / T::kStep;
+    const int mine = n0 < s.N && nst > kk ? (nst - kk + wk - 1) / wk : 0;
+    const __amdgpu_buffer_rsrc_t rw = thin_rsrc(s.W, s.w_bytes);
+    const __amdgpu_buffer_rsrc_t ra = thin_rsrc(s.A, s.a_bytes);
+    uint32_t row[MB];
+#pragma unroll
+    for (int m = 0; m < MB; ++m) {
+        const int i = m * 16 + (lane & 15);
+        row[m] = i < nrows ? (uint32_t)src(i) * (uint32_t)s.lda : kThinDrop;
+    }
+    f32x4 acc[MB][T::kAcc];
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+        for (int q = 0; q < T::kAcc; ++q) acc[m][q] = f32x4{0.f, 0.f, 0.f, 0.f};
+    T w[P];
+    typename T::template A<MB> a[P];
+    auto load = [&](int slot, int i) {
+        const int k = (kk + wk * i) * T::kStep;
+        w[slot].load(rw, s, n0, k, lane);
+        a[slot].load(ra, row, k, s.Kd, lane);
+    };
+#pragma unroll
+    for (int q = 0; q < P; ++q)
+        if (q < mine) load(q, q);
+    for (int i0 = 0; i0 < mine; i0 += P) {
+#pragma unroll
+        for (int q = 0; q < P; ++q) {
+            if (i0 + q >= mine) break;
+            w[q].template mma<MB>(acc, a[q]);
+            if (i0 + q + P < mine) load(q, i0 + q + P);
+        }
+    }
+    auto leave = [&](int m, int v, f32x4 t) {
+        const int i = m * 16 + (lane & 15), col = n0 + T::piece_col(v, lane);
+        if (i >= nrows || col >= s.N) return;   // N is a multiple of 8
+        if constexpr (T::kI8) {
+            const float rs = s.row_scale[src(i)];
+            const f32x4 cs = *(const f32x4*)(s.col_scale + col);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) t[q] = (float)__float_as_int(t[q]) * rs * cs[q];
+        }
+        const int64_t at = (int64_t)dst(i) * s.N + col;
+        if (s.epi == THIN_F32) {
+            *(f32x4*)((float*)s.out + at) = t;
+        } else {
+            if (s.epi == THIN_RELU2) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    t[q] = relu_f32(t[q]);
+                    t[q] *= t[q];
+                }
+            }
+            *(u32x2_thin*)((uint16_t*)s.out + at) = u32x2_thin{pack_bf16x2(t[0], t[1]), pack_bf16x2(t[2], t[3])};
+        }
+    };
+#pragma unroll
+    for (int m = 0; m < MB; ++m) {
+        if (m > 0 && m * 16 >= nrows) break;
+        if (wk == 1) {
+#pragma unroll
+            for (int v = 0; v < T::kAcc; ++v) leave(m, v, T::piece(acc[m], v));
+        } else {
+            if (m > 0) __syncthreads();
+#pragma unroll
+            for (int v = 0; v < T::kAcc; ++v) red[wave][v][lane] = T::piece(acc[m], v);
+            __syncthreads();
+            const int first = wave - kk;
+            for (int v = kk; v < T::kAcc; v += wk) {
+                f32x4 t = red[first][v][lane];
+                for (int j = 1; j < wk; ++j) t = thin_add<T::kI8>(t, red[first + j][v][lane]);
+                leave(m, v, t);
+            }
+        }
+    }
+}
+
+// thin_body for as few 16-row blocks as nrows needs, of at most MBMAX.
+template <class T, int MBMAX, class Src, class Dst>
+__device__ __forceinline__ void thin_rows(const ThinArgs& s, int n0, int kk, int wk, int nrows, Src&& src, Dst&& dst,
+                                          f32x4 (*red)[T::kAcc][64]) {
+    if (MBMAX == 1 || nrows <= 16) thin_body<T, 1>(s, n0, kk, wk, nrows, src, dst, red);
+    else if (MBMAX == 2 || nrows <= 32) thin_body<T, MBMAX == 1 ? 1 : 2>(s, n0, kk, wk, nrows, src, dst, red);
+    else thin_body<T, MBMAX>(s, n0, kk, wk, nrows, src, dst, red);
+}
+
+}  // namespace moe

@@ -139,8 +139,9 @@ def test_grouped_gemm_i8(counts, Kd, N, epilogue):
         assert bool(((C[a:b].double() - ref).abs() <= ref.abs() * ROUND).all()), e
 
 
-@pytest.mark.parametrize("M, Kd, N", [(0, 16, 8), (1, 16, 8), (5, 2688, 672), (127, 48, 264), (129, 1040, 72),
-                                      (4100, 336, 1024), (9000, 2064, 1288)])
+@pytest.mark.parametrize("M, Kd, N", [(0, 16, 8), (1, 16, 8), (5, 2688, 672), (16, 4096, 40), (17, 336, 1024),
+                                      (32, 4096, 72), (31, 4080, 8), (32, 4112, 24), (33, 272, 104), (127, 48, 264),
+                                      (129, 1040, 72), (4100, 336, 1024), (9000, 2064, 1288)])
 def test_latent_proj_i8(M, Kd, N):
     g = gen(M + N)
     A, W = randn(g, M, Kd), randn(g, Kd, N, std=Kd ** -0.5)
