@@ -8,6 +8,7 @@
 //   few_logits   partial router logits: 64 d x 64 experts x 16 tokens a workgroup, fp32 products
 //   few_route    one workgroup a token: the partial sums, top-K and weights; with 8-bit
 //                weights as many again quantise the token rows
+//   few_table    many picks: the picked experts' rows, else found by each workgroup below
 //   few_gemm     up: h = bf16(max(x W1, 0)^2)
 //   few_quant    8-bit weights: the rows of h
 //   few_gemm     down: y_k = h W2 in fp32
@@ -247,6 +248,8 @@ struct FewSide {
 struct FewGemmArgs {
     FewSide routed, shared;
     const int32_t* idx;   // [S, K]
+    const int4* table;    // the picked experts {expert, first in rows, rows, 0}, from few_table; null: each workgroup
+    const int32_t* rows;  // searches the picks itself
     int S, K, r_items;    // workgroups of the routed experts
     int wk;               // waves that share a slab's contraction; 4 / wk slabs side by side in a workgroup
     int epi;
@@ -304,6 +307,60 @@ __device__ __forceinline__ int few_plan(const int32_t* __restrict__ idx, int S, 
     return e;
 }
 
+// The picked experts, ascending, and their rows, by one workgroup: entries of table past
+// them hold no rows.  An expert's rows come in any order: a row's result depends on the
+// row alone.
+constexpr int kTableThreads = 1024;
+__global__ __launch_bounds__(kTableThreads) void few_table_kernel(const int32_t* __restrict__ idx, int n, int entries,
+                                                                  int4* __restrict__ table, int32_t* __restrict__ rows) {
+    __shared__ int32_t count[kMaxExperts], first[kMaxExperts];
+    __shared__ int2 wsum[kTableThreads / 64];
+    const int e = threadIdx.x, lane = e & 63, wave = e >> 6;
+    count[e] = 0;
+    __syncthreads();
+    int pick[2], rank[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {   // n <= 64 x 32
+        const int q = e + u * kTableThreads;
+        if (q < n) {
+            pick[u] = idx[q] & (kMaxExperts - 1);
+            rank[u] = atomicAdd(&count[pick[u]], 1);
+        }
+    }
+    __syncthreads();
+    const int c = min(count[e], kFewMaxTokens);   // a token picks an expert once
+    int2 incl = make_int2(c, c > 0 ? 1 : 0);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int ox = __shfl_up(incl.x, d), oy = __shfl_up(incl.y, d);
+        if (lane >= d) {
+            incl.x += ox;
+            incl.y += oy;
+        }
+    }
+    if (lane == 63) wsum[wave] = incl;
+    __syncthreads();
+    int2 base = make_int2(0, 0);
+    int active = 0;
+    for (int w = 0; w < kTableThreads / 64; ++w) {
+        if (w < wave) {
+            base.x += wsum[w].x;
+            base.y += wsum[w].y;
+        }
+        active += wsum[w].y;
+    }
+    const int f = base.x + incl.x - c;
+    first[e] = f;
+    if (c > 0) table[base.y + incl.y - 1] = make_int4(e, f, c, 0);
+    if (e >= active && e < entries) table[e] = make_int4(0, 0, 0, 0);
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int q = e + u * kTableThreads;
+        if (q < n && rank[u] < kFewMaxTokens) rows[first[pick[u]] + rank[u]] = q;
+    }
+}
+
 // MBMAX = 1: at most 16 tokens, so at most 16 rows an expert; four waves a SIMD.
 template <class T, int MBMAX>
 __global__ __launch_bounds__(kFewThreads, MBMAX == 1 ? 4 : 2) void few_gemm_kernel(FewGemmArgs p) {
@@ -313,22 +370,27 @@ __global__ __launch_bounds__(kFewThreads, MBMAX == 1 ? 4 : 2) void few_gemm_kern
     const int b = (int)blockIdx.x - (shared ? p.r_items : 0);
     const FewSide s = shared ? p.shared : p.routed;
     const int a = b / s.groups, in = b - a * s.groups;
-    int e = 0;
-    if (shared) {
-        if ((int)threadIdx.x < p.S) sh.rows[threadIdx.x] = threadIdx.x;
-        if (threadIdx.x == 0) sh.nrows = p.S;
-    } else {
+    int e = 0, nrows = p.S;
+    const int32_t* rows = nullptr;   // the shared expert's are the tokens
+    if (!shared && p.table != nullptr) {
+        const int4 t = p.table[a];
+        e = __builtin_amdgcn_readfirstlane(t.x);
+        nrows = __builtin_amdgcn_readfirstlane(t.z);
+        if (nrows == 0) return;
+        rows = p.rows + __builtin_amdgcn_readfirstlane(t.y);
+    } else if (!shared) {
         e = few_plan(p.idx, p.S, p.K, a, sh);
         if (e < 0) return;
+        __syncthreads();
+        nrows = __builtin_amdgcn_readfirstlane(sh.nrows);
+        rows = sh.rows;
     }
-    __syncthreads();
-    const int nrows = __builtin_amdgcn_readfirstlane(sh.nrows);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wk = p.wk;
     const int kk = wave & (wk - 1), n0 = (in * (4 / wk) + wave / wk) * T::kCols;
     const ThinArgs t{s.A, (const char*)s.W + e * s.w_bytes, s.out, s.row_scale, s.col_scale + (int64_t)e * s.N,
                      s.a_bytes, s.w_bytes, s.lda, s.Kd, s.N, p.epi};
-    thin_rows<T, MBMAX>(t, n0, kk, wk, nrows, [&](int i) { return sh.rows[i] / s.a_div; },
-                        [&](int i) { return sh.rows[i]; }, red);
+    thin_rows<T, MBMAX>(t, n0, kk, wk, nrows, [&](int r) { return r / s.a_div; },
+                        [&](int i) { return rows != nullptr ? rows[i] : i; }, red);
 }
 
 // ---- between the products and after them ------------------------------------
@@ -421,25 +483,36 @@ int cdiv(int a, int b) { return (a + b - 1) / b; }
 struct FewPlan {
     int nd, r_experts;
     int wk1, wk2;          // waves that share a slab of the up and of the down product
-    size_t part, idx, prob, xq, xs, h, hs, hq, hqs, sc, scs, y, ys, bytes;   // offsets
+    bool table;
+    size_t part, idx, prob, tab, rows, xq, xs, h, hs, hq, hqs, sc, scs, y, ys, bytes;   // offsets
 };
 
 // Waves of a workgroup's four that share a slab's contraction, each keeping a step.  Four
-// give the most workgroups, which the CUs then share evenly (us with 1 / 2 / 4, one product's
-// choice varied: 8 tokens of 192 experts 382 / 354 / 347; 1 token of 64 40 / 31 / 26.5); with many
-// picks two, since every workgroup searches them all (64 tokens of 64 experts: 116 / 119 / 121
-// and 119 / 120 / 127; 32 of 256: 302 / 290 / 283 and 303 / 300 / 314).
-int few_share(int picks, int steps) {
-    const int most = picks > 256 ? 2 : 4;
-    return std::min(most, steps >= 4 ? 4 : steps >= 2 ? 2 : 1);
+// give the most workgroups, which the CUs then share evenly, two the fewer that have to find
+// their rows and join their sums: two where they still make two workgroups a CU of more than
+// 16 tokens (us with 2 / 4: 64 tokens top-6 of 64 experts 121 / 129, top-22 of 512 422 / 440 and in 8
+// bits 251 / 280, but top-2 of 8 88 / 78), and with up to 16 tokens and bf16 weights eight a CU
+// (16 tokens top-8 of 256 349 / 361; 8 tokens of the 192-expert layer 354 / 347, one product's
+// choice varied; 1 token of 64 31 / 26.5; 16 tokens top-8 of 256 in 8 bits 193 / 189).
+int few_share(bool i8, bool many, int slabs, int steps) {
+    const int groups = many ? 2 : i8 ? 1 << 20 : 8;   // a CU's
+    int wk = slabs / 2 >= (int64_t)groups * cu_count() ? 2 : 4;
+    while (wk > steps) wk /= 2;
+    return wk;
 }
 
-// Columns of a slab.  8-bit weights take 32, or with more than 16 tokens 64, which halves
-// how often the workgroups read the rows (64 tokens of 64 experts 86 -> 78 us; 16 tokens
-// of 256: 186.4 with 32, 189.3 with 64).
+// Whether a launch of its own (2.5 us) finds the picked experts' rows, instead of every
+// workgroup of both products.  64 tokens top-22 of 512 422 us against 459 and, in 8 bits, 251
+// against 330; 40 tokens top-22 of 64 51 / 54; 64 tokens top-6 of 64 (384 picks) 121 / 121; 16 tokens
+// top-8 of 256 (128 picks) 349 / 348.
+bool few_table_pays(int picks) { return picks > 256; }
+
+// Columns of a slab.  8-bit weights take 32, or, where more than 16 tokens give an expert
+// several rows, 64, which halves how often they are read (us with 32 / 64: 64 tokens top-6 of
+// 64 81 / 77, top-2 of 8 57 / 53; top-22 of 512 251 / 267; 16 tokens top-8 of 256 189 / 192).
 int few_cols(const moe_layer_few_args* a) {
     if (a->weights != MOE_WEIGHTS_I8) return ThinBf16::kCols;
-    return a->S <= 16 ? ThinI8<2>::kCols : ThinI8<4>::kCols;
+    return a->S > 16 && a->S * a->K >= 4 * (int64_t)a->E ? ThinI8<4>::kCols : ThinI8<2>::kCols;
 }
 
 FewPlan few_plan_of(const moe_layer_few_args* a) {
@@ -450,8 +523,9 @@ FewPlan few_plan_of(const moe_layer_few_args* a) {
     const int step = i8 ? ThinI8<2>::kStep : ThinBf16::kStep;
     p.nd = cdiv(D, kFewD);
     p.r_experts = (int)std::min<size_t>((size_t)E, R);
-    p.wk1 = few_share((int)R, cdiv(D, step));
-    p.wk2 = few_share((int)R, cdiv(F, step));
+    const int cols = few_cols(a), ns = Fs ? 1 : 0;
+    p.wk1 = few_share(i8, S > 16, p.r_experts * cdiv(F, cols) + ns * cdiv(Fs, cols), cdiv(D, step));
+    p.wk2 = few_share(i8, S > 16, (p.r_experts + ns) * cdiv(D, cols), cdiv(F, step));
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t o = at;
@@ -461,6 +535,9 @@ FewPlan few_plan_of(const moe_layer_few_args* a) {
     p.part = take((size_t)p.nd * S * E * 4);
     p.idx = take(R * 4);
     p.prob = take(R * 4);
+    p.table = few_table_pays((int)R);
+    p.tab = take(p.table ? (size_t)p.r_experts * 16 : 0);
+    p.rows = take(p.table ? R * 4 : 0);
     p.xq = take(i8 ? (size_t)S * D : 0);
     p.xs = take((size_t)S * 4);
     p.h = take(R * F * 2);
@@ -514,6 +591,10 @@ hipError_t launch_layer_few(const moe_layer_few_args* a, hipStream_t st) {
     else if (E <= 512) launch_route_few<8>(sig, gr, st, part, p.nd, a, idx, prob, xq, xs);
     else launch_route_few<16>(sig, gr, st, part, p.nd, a, idx, prob, xq, xs);
 
+    const int4* table = p.table ? (const int4*)(ws + p.tab) : nullptr;
+    if (p.table)
+        hipLaunchKernelGGL(few_table_kernel, dim3(1), dim3(kTableThreads), 0, st, idx, R, p.r_experts,
+                           (int4*)(ws + p.tab), (int32_t*)(ws + p.rows));
     auto gemm = [&](FewSide r, FewSide s, int wk, int epi) {
         for (FewSide* q : {&r, &s}) {
             q->lda = q->Kd * wb;
@@ -522,13 +603,14 @@ hipError_t launch_layer_few(const moe_layer_few_args* a, hipStream_t st) {
             q->groups = cdiv(cdiv(q->N, cols), 4 / wk);
         }
         if (Fs == 0) s.groups = 0;
-        const FewGemmArgs g{r, s, idx, S, K, p.r_experts * r.groups, wk, epi};
+        const FewGemmArgs g{r, s, idx, table, (const int32_t*)(ws + p.rows), S, K, p.r_experts * r.groups, wk, epi};
         const dim3 grid((unsigned)(g.r_items + s.groups)), block(kFewThreads);
         if (S <= 16) {
             if (i8) hipLaunchKernelGGL((few_gemm_kernel<ThinI8<2>, 1>), grid, block, 0, st, g);
             else hipLaunchKernelGGL((few_gemm_kernel<ThinBf16, 1>), grid, block, 0, st, g);
         } else {
-            if (i8) hipLaunchKernelGGL((few_gemm_kernel<ThinI8<4>, 4>), grid, block, 0, st, g);
+            if (i8 && cols == 64) hipLaunchKernelGGL((few_gemm_kernel<ThinI8<4>, 4>), grid, block, 0, st, g);
+            else if (i8) hipLaunchKernelGGL((few_gemm_kernel<ThinI8<2>, 4>), grid, block, 0, st, g);
             else hipLaunchKernelGGL((few_gemm_kernel<ThinBf16, 4>), grid, block, 0, st, g);
         }
     };

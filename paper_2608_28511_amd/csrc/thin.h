@@ -145,8 +145,8 @@ __device__ __forceinline__ f32x4 thin_add(f32x4 a, f32x4 b) {
         return a + b;
 }
 
-// Columns [n0, n0 + kCols) of the product for 16 MB rows, of which nrows exist: src(i) is
-// row i's place in A and dst(i) its row in out.  The wave is the kk-th of the wk that share
+// Columns [n0, n0 + kCols) of the product for 16 MB rows, of which nrows exist: dst(i) is
+// row i's row in out and src(dst) its place in A.  The wave is the kk-th of the wk that share
 // the slab: it takes every wk-th step, and their sums are joined through LDS in wave
 // order, each wave finishing some of the slab's pieces.  Every wave of the workgroup calls
 // it (n0 may lie past N: such a slab has nothing to do).
@@ -159,12 +159,6 @@ __device__ __forceinline__ void thin_body(const ThinArgs& s, int n0, int kk, int
     const int mine = n0 < s.N && nst > kk ? (nst - kk + wk - 1) / wk : 0;
     const __amdgpu_buffer_rsrc_t rw = thin_rsrc(s.W, s.w_bytes);
     const __amdgpu_buffer_rsrc_t ra = thin_rsrc(s.A, s.a_bytes);
-    uint32_t row[MB];
-#pragma unroll
-    for (int m = 0; m < MB; ++m) {
-        const int i = m * 16 + (lane & 15);
-        row[m] = i < nrows ? (uint32_t)src(i) * (uint32_t)s.lda : kThinDrop;
-    }
     f32x4 acc[MB][T::kAcc];
 #pragma unroll
     for (int m = 0; m < MB; ++m)
@@ -172,32 +166,44 @@ __device__ __forceinline__ void thin_body(const ThinArgs& s, int n0, int kk, int
         for (int q = 0; q < T::kAcc; ++q) acc[m][q] = f32x4{0.f, 0.f, 0.f, 0.f};
     T w[P];
     typename T::template A<MB> a[P];
-    auto load = [&](int slot, int i) {
-        const int k = (kk + wk * i) * T::kStep;
-        w[slot].load(rw, s, n0, k, lane);
-        a[slot].load(ra, row, k, s.Kd, lane);
-    };
+    auto step_k = [&](int i) { return (kk + wk * i) * T::kStep; };
+    // the weights' first steps are on their way before the rows are known
 #pragma unroll
     for (int q = 0; q < P; ++q)
-        if (q < mine) load(q, q);
+        if (q < mine) w[q].load(rw, s, n0, step_k(q), lane);
+    int to[MB], from[MB];
+    uint32_t row[MB];
+#pragma unroll
+    for (int m = 0; m < MB; ++m) {
+        const int i = m * 16 + (lane & 15);
+        to[m] = i < nrows ? dst(i) : -1;
+        from[m] = i < nrows ? src(to[m]) : 0;
+        row[m] = i < nrows ? (uint32_t)from[m] * (uint32_t)s.lda : kThinDrop;
+    }
+#pragma unroll
+    for (int q = 0; q < P; ++q)
+        if (q < mine) a[q].load(ra, row, step_k(q), s.Kd, lane);
     for (int i0 = 0; i0 < mine; i0 += P) {
 #pragma unroll
         for (int q = 0; q < P; ++q) {
             if (i0 + q >= mine) break;
             w[q].template mma<MB>(acc, a[q]);
-            if (i0 + q + P < mine) load(q, i0 + q + P);
+            if (i0 + q + P < mine) {
+                w[q].load(rw, s, n0, step_k(i0 + q + P), lane);
+                a[q].load(ra, row, step_k(i0 + q + P), s.Kd, lane);
+            }
         }
     }
     auto leave = [&](int m, int v, f32x4 t) {
-        const int i = m * 16 + (lane & 15), col = n0 + T::piece_col(v, lane);
-        if (i >= nrows || col >= s.N) return;   // N is a multiple of 8
+        const int col = n0 + T::piece_col(v, lane);
+        if (to[m] < 0 || col >= s.N) return;   // N is a multiple of 8
         if constexpr (T::kI8) {
-            const float rs = s.row_scale[src(i)];
+            const float rs = s.row_scale[from[m]];
             const f32x4 cs = *(const f32x4*)(s.col_scale + col);
 #pragma unroll
             for (int q = 0; q < 4; ++q) t[q] = (float)__float_as_int(t[q]) * rs * cs[q];
         }
-        const int64_t at = (int64_t)dst(i) * s.N + col;
+        const int64_t at = (int64_t)to[m] * s.N + col;
         if (s.epi == THIN_F32) {
             *(f32x4*)((float*)s.out + at) = t;
         } else {
