@@ -24,6 +24,7 @@
 namespace moe {
 
 constexpr int kFewThreads = kThinThreads;
+constexpr int kSlabBf16 = ThinBf16<false>::kCols, kSlabI8 = ThinI8<2, false>::kCols;
 static_assert(kFewMaxTokens <= kThinRows, "an expert's rows are at most the tokens");
 
 // ---- router ---------------------------------------------------------------
@@ -365,7 +366,7 @@ __global__ __launch_bounds__(kTableThreads) void few_table_kernel(const int32_t*
 template <class T, int MBMAX>
 __global__ __launch_bounds__(kFewThreads, MBMAX == 1 ? 4 : 2) void few_gemm_kernel(FewGemmArgs p) {
     __shared__ FewPicks sh;
-    __shared__ f32x4 red[4][T::kAcc][64];   // wk > 1: every wave's sums
+    __shared__ __attribute__((aligned(16))) char lds[4 * T::kWaveLds];
     const bool shared = (int)blockIdx.x >= p.r_items;
     const int b = (int)blockIdx.x - (shared ? p.r_items : 0);
     const FewSide s = shared ? p.shared : p.routed;
@@ -390,7 +391,7 @@ __global__ __launch_bounds__(kFewThreads, MBMAX == 1 ? 4 : 2) void few_gemm_kern
     const ThinArgs t{s.A, (const char*)s.W + e * s.w_bytes, s.out, s.row_scale, s.col_scale + (int64_t)e * s.N,
                      s.a_bytes, s.w_bytes, s.lda, s.Kd, s.N, p.epi};
     thin_rows<T, MBMAX>(t, n0, kk, wk, nrows, [&](int r) { return r / s.a_div; },
-                        [&](int i) { return rows != nullptr ? rows[i] : i; }, red);
+                        [&](int i) { return rows != nullptr ? rows[i] : i; }, lds);
 }
 
 // ---- between the products and after them ------------------------------------
@@ -511,8 +512,8 @@ bool few_table_pays(int picks) { return picks > 256; }
 // several rows, 64, which halves how often they are read (us with 32 / 64: 64 tokens top-6 of
 // 64 81 / 77, top-2 of 8 57 / 53; top-22 of 512 251 / 267; 16 tokens top-8 of 256 189 / 192).
 int few_cols(const moe_layer_few_args* a) {
-    if (a->weights != MOE_WEIGHTS_I8) return ThinBf16::kCols;
-    return a->S > 16 && a->S * a->K >= 4 * (int64_t)a->E ? ThinI8<4>::kCols : ThinI8<2>::kCols;
+    if (a->weights != MOE_WEIGHTS_I8) return kSlabBf16;
+    return a->S > 16 && a->S * a->K >= 4 * (int64_t)a->E ? 2 * kSlabI8 : kSlabI8;
 }
 
 FewPlan few_plan_of(const moe_layer_few_args* a) {
@@ -520,7 +521,7 @@ FewPlan few_plan_of(const moe_layer_few_args* a) {
     const int S = (int)a->S, D = a->D, E = a->E, K = a->K, F = a->F, Fs = a->Fs;
     const bool i8 = a->weights == MOE_WEIGHTS_I8;
     const size_t R = (size_t)S * K;
-    const int step = i8 ? ThinI8<2>::kStep : ThinBf16::kStep;
+    const int step = i8 ? ThinI8<2, false>::kStep : ThinBf16<false>::kStep;
     p.nd = cdiv(D, kFewD);
     p.r_experts = (int)std::min<size_t>((size_t)E, R);
     const int cols = few_cols(a), ns = Fs ? 1 : 0;
@@ -605,14 +606,15 @@ hipError_t launch_layer_few(const moe_layer_few_args* a, hipStream_t st) {
         if (Fs == 0) s.groups = 0;
         const FewGemmArgs g{r, s, idx, table, (const int32_t*)(ws + p.rows), S, K, p.r_experts * r.groups, wk, epi};
         const dim3 grid((unsigned)(g.r_items + s.groups)), block(kFewThreads);
-        if (S <= 16) {
-            if (i8) hipLaunchKernelGGL((few_gemm_kernel<ThinI8<2>, 1>), grid, block, 0, st, g);
-            else hipLaunchKernelGGL((few_gemm_kernel<ThinBf16, 1>), grid, block, 0, st, g);
-        } else {
-            if (i8 && cols == 64) hipLaunchKernelGGL((few_gemm_kernel<ThinI8<4>, 4>), grid, block, 0, st, g);
-            else if (i8) hipLaunchKernelGGL((few_gemm_kernel<ThinI8<2>, 4>), grid, block, 0, st, g);
-            else hipLaunchKernelGGL((few_gemm_kernel<ThinBf16, 4>), grid, block, 0, st, g);
-        }
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, g); };
+        auto pick = [&](auto nt) {
+            constexpr bool NT = decltype(nt)::value;
+            if (S <= 16) i8 ? go(few_gemm_kernel<ThinI8<2, NT>, 1>) : go(few_gemm_kernel<ThinBf16<NT>, 1>);
+            else if (!i8) go(few_gemm_kernel<ThinBf16<NT>, 4>);
+            else cols == kSlabI8 ? go(few_gemm_kernel<ThinI8<2, NT>, 4>) : go(few_gemm_kernel<ThinI8<4, NT>, 4>);
+        };
+        if (thin_nt(r.W, (int64_t)(i8 ? r.Kd : r.N) * wb, 2 * (int64_t)p.r_experts * r.w_bytes)) pick(std::true_type{});
+        else pick(std::false_type{});
     };
     // A, W, out, row and column scales, rows of A, .., .., a_div, Kd, N (the rest is set above)
     const void* x = i8 ? (const void*)xq : (const void*)a->x;

@@ -14,6 +14,7 @@
 namespace moe {
 
 constexpr uint32_t kThinDrop = 0x80000000u;   // beyond any descriptor's range: reads as zero
+constexpr int kThinNt = 2;                   // cache policy: non-temporal
 constexpr int kThinThreads = 256;
 constexpr int kThinRows = 64;
 typedef unsigned u32x2_thin __attribute__((ext_vector_type(2)));
@@ -40,10 +41,13 @@ struct ThinArgs {
 
 // bf16 weights, N-contiguous: slabs of 64 columns, steps of 32 k.  A lane loads 4
 // columns of 8 k rows (each load of the wave four whole cache lines) and packs them into
-// the fragments of columns 4 c + q, q = 0 .. 3, with one byte permutation a register.
+// the fragments of columns 4 c + q, q = 0 .. 3, with one byte permutation a register.  NT:
+// non-temporal loads (see thin_nt).
+template <bool NT>
 struct ThinBf16 {
     static constexpr bool kI8 = false;
     static constexpr int kCols = 64, kStep = 32, kAcc = 4;
+    static constexpr int kWaveLds = kAcc * 1024;   // bytes: the wave's sums
     template <int MB>
     static constexpr int kAhead = MB == 4 ? 3 : 4;
     u32x2_thin w[8];
@@ -53,7 +57,7 @@ struct ThinBf16 {
         const uint32_t ld = (uint32_t)s.N * 2;
         const uint32_t o = n0 + 4 * c < s.N ? (uint32_t)(k + 8 * g) * ld + (uint32_t)(n0 + 4 * c) * 2 : kThinDrop;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = __builtin_amdgcn_raw_buffer_load_b64(rw, o + (uint32_t)j * ld, 0, 0);
+        for (int j = 0; j < 8; ++j) w[j] = __builtin_amdgcn_raw_buffer_load_b64(rw, o + (uint32_t)j * ld, 0, NT ? kThinNt : 0);
     }
     template <int MB>
     struct A {
@@ -67,7 +71,7 @@ struct ThinBf16 {
         }
     };
     template <int MB>
-    __device__ __forceinline__ void mma(f32x4 (&acc)[MB][kAcc], const A<MB>& a) const {
+    __device__ __forceinline__ void mma(f32x4 (&acc)[MB][kAcc], const A<MB>& a, char*) const {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             u32x4 f;
@@ -86,25 +90,31 @@ struct ThinBf16 {
     __device__ __forceinline__ static int piece_col(int v, int lane) { return 16 * (lane >> 4) + 4 * v; }
 };
 
-// 8-bit weights, K-contiguous: slabs of 16 NB columns, steps of 128 k, whose fragments
-// are 16 bytes of a channel as they lie in memory.
-template <int NB>
+// 8-bit weights, K-contiguous: slabs of 16 NB columns, steps of 128 k.  A fragment is 16
+// bytes of each of 16 channels and four places: loaded as such, an instruction takes half of
+// 16 cache lines.  NT: it takes eight whole ones, non-temporally, which the wave turns into
+// fragments in 2 NB KB of LDS of its own (row layout of tile_dma.h).  Half lines were fetched
+// twice non-temporally (16 tokens top-8 of 256: 185 us as they lie in memory, 204 with the
+// hint, 164 with whole lines and the hint), and whole lines alone cost the turn (3 tokens
+// top-22 of 512: 53 / 59).  Two steps ahead: three cost a workgroup a CU (53 / 55.5).
+template <int NB, bool NT>
 struct ThinI8 {
     static constexpr bool kI8 = true;
     static constexpr int kCols = 16 * NB, kStep = 128, kAcc = NB;
+    static constexpr int kWaveLds = NB * 2048;
     template <int MB>
-    static constexpr int kAhead = MB == 4 || NB == 4 ? 2 : 3;
+    static constexpr int kAhead = 2;
     u32x4 w[NB][2];
 
     __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t& rw, const ThinArgs& s, int n0, int k, int lane) {
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            const int n = n0 + 16 * b + (lane & 15);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int kk = k + 64 * h + 16 * (lane >> 4);
+                const int n = n0 + 16 * b + (NT ? 8 * h + (lane >> 3) : lane & 15);
+                const int kk = k + (NT ? 16 * (lane & 7) : 64 * h + 16 * (lane >> 4));
                 const uint32_t o = n < s.N && kk < s.Kd ? (uint32_t)n * (uint32_t)s.Kd + (uint32_t)kk : kThinDrop;
-                w[b][h] = __builtin_amdgcn_raw_buffer_load_b128(rw, o, 0, 0);
+                w[b][h] = __builtin_amdgcn_raw_buffer_load_b128(rw, o, 0, NT ? kThinNt : 0);
             }
         }
     }
@@ -122,15 +132,42 @@ struct ThinI8 {
                 }
         }
     };
+    // stage: the wave's LDS
     template <int MB>
-    __device__ __forceinline__ void mma(f32x4 (&acc)[MB][kAcc], const A<MB>& a) const {
+    __device__ __forceinline__ void mma(f32x4 (&acc)[MB][kAcc], const A<MB>& a, char* stage) const {
+        const int lane = threadIdx.x & 63;
+        u32x4 f[NB][2];
+        if constexpr (NT) {
+            // a wave's LDS operations are in order: no barrier between its writes and reads
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int r = 8 * h + (lane >> 3);
+                    *(u32x4*)(stage + b * 2048 + r * 128 + (((lane & 7) ^ rswz(r)) * 16)) = w[b][h];
+                }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int r = lane & 15, c = 4 * h + (lane >> 4);
+                    f[b][h] = *(const u32x4*)(stage + b * 2048 + r * 128 + ((c ^ rswz(r)) * 16));
+                }
+            __builtin_amdgcn_wave_barrier();
+        } else {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) f[b][h] = w[b][h];
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int m = 0; m < MB; ++m)
-                    acc[m][b] = mfma16<true>(__builtin_bit_cast(bf16x8, w[b][h]), __builtin_bit_cast(bf16x8, a.v[m][h]),
+                    acc[m][b] = mfma16<true>(__builtin_bit_cast(bf16x8, f[b][h]), __builtin_bit_cast(bf16x8, a.v[m][h]),
                                              acc[m][b]);
     }
     __device__ __forceinline__ static f32x4 piece(const f32x4 (&acc)[kAcc], int b) { return acc[b]; }
@@ -148,11 +185,11 @@ __device__ __forceinline__ f32x4 thin_add(f32x4 a, f32x4 b) {
 // Columns [n0, n0 + kCols) of the product for 16 MB rows, of which nrows exist: dst(i) is
 // row i's row in out and src(dst) its place in A.  The wave is the kk-th of the wk that share
 // the slab: it takes every wk-th step, and their sums are joined through LDS in wave
-// order, each wave finishing some of the slab's pieces.  Every wave of the workgroup calls
-// it (n0 may lie past N: such a slab has nothing to do).
+// order, each wave finishing some of the slab's pieces.  lds: T::kWaveLds bytes of every wave.
+// Every wave of the workgroup calls it (n0 may lie past N: such a slab has nothing to do).
 template <class T, int MB, class Src, class Dst>
 __device__ __forceinline__ void thin_body(const ThinArgs& s, int n0, int kk, int wk, int nrows, Src&& src, Dst&& dst,
-                                          f32x4 (*red)[T::kAcc][64]) {
+                                          char* lds) {
     constexpr int P = T::template kAhead<MB>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int nst = (s.Kd + T::kStep - 1) / T::kStep;
@@ -187,7 +224,7 @@ __device__ __forceinline__ void thin_body(const ThinArgs& s, int n0, int kk, int
 #pragma unroll
         for (int q = 0; q < P; ++q) {
             if (i0 + q >= mine) break;
-            w[q].template mma<MB>(acc, a[q]);
+            w[q].template mma<MB>(acc, a[q], lds + wave * T::kWaveLds);
             if (i0 + q + P < mine) {
                 w[q].load(rw, s, n0, step_k(i0 + q + P), lane);
                 a[q].load(ra, row, step_k(i0 + q + P), s.Kd, lane);
@@ -225,26 +262,38 @@ __device__ __forceinline__ void thin_body(const ThinArgs& s, int n0, int kk, int
             for (int v = 0; v < T::kAcc; ++v) leave(m, v, T::piece(acc[m], v));
         } else {
             if (m > 0) __syncthreads();
+            auto sum = [&](int w, int v) -> f32x4& { return ((f32x4*)(lds + w * T::kWaveLds))[v * 64 + lane]; };
 #pragma unroll
-            for (int v = 0; v < T::kAcc; ++v) red[wave][v][lane] = T::piece(acc[m], v);
+            for (int v = 0; v < T::kAcc; ++v) sum(wave, v) = T::piece(acc[m], v);
             __syncthreads();
             const int first = wave - kk;
             for (int v = kk; v < T::kAcc; v += wk) {
-                f32x4 t = red[first][v][lane];
-                for (int j = 1; j < wk; ++j) t = thin_add<T::kI8>(t, red[first + j][v][lane]);
+                f32x4 t = sum(first, v);
+                for (int j = 1; j < wk; ++j) t = thin_add<T::kI8>(t, sum(first + j, v));
                 leave(m, v, t);
             }
         }
     }
 }
 
+// Whether weights [rows, row_bytes] at W, of which a call reads `bytes` in all, are better
+// read non-temporally: not what the last-level cache (256 MB) may still hold from the call
+// before, and not where rows do not start on cache lines, parts of which such loads fetch
+// twice (us, without / with the hint, bf16: 64 tokens of 64 experts, 537 MB, 119 / 105; 8 of the
+// 192-expert layer, 2.1 GB, 320 / 289; 1 token of 64, 50 MB, 25.5 / 29.5; 1 token top-22 of 512,
+// 110 MB, 39 / 41; 64 tokens top-22 of 512, rows of 1,344 bytes among them, 423 / 431 and, those
+// excepted, 403).
+inline bool thin_nt(const void* W, int64_t row_bytes, int64_t bytes) {
+    return bytes > (int64_t)256 << 20 && row_bytes % 128 == 0 && (uintptr_t)W % 128 == 0;
+}
+
 // thin_body for as few 16-row blocks as nrows needs, of at most MBMAX.
 template <class T, int MBMAX, class Src, class Dst>
 __device__ __forceinline__ void thin_rows(const ThinArgs& s, int n0, int kk, int wk, int nrows, Src&& src, Dst&& dst,
-                                          f32x4 (*red)[T::kAcc][64]) {
-    if (MBMAX == 1 || nrows <= 16) thin_body<T, 1>(s, n0, kk, wk, nrows, src, dst, red);
-    else if (MBMAX == 2 || nrows <= 32) thin_body<T, MBMAX == 1 ? 1 : 2>(s, n0, kk, wk, nrows, src, dst, red);
-    else thin_body<T, MBMAX>(s, n0, kk, wk, nrows, src, dst, red);
+                                          char* lds) {
+    if (MBMAX == 1 || nrows <= 16) thin_body<T, 1>(s, n0, kk, wk, nrows, src, dst, lds);
+    else if (MBMAX == 2 || nrows <= 32) thin_body<T, MBMAX == 1 ? 1 : 2>(s, n0, kk, wk, nrows, src, dst, lds);
+    else thin_body<T, MBMAX>(s, n0, kk, wk, nrows, src, dst, lds);
 }
 
 }  // namespace moe

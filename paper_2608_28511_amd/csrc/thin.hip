@@ -11,13 +11,15 @@
 namespace moe {
 
 constexpr int kProjWaves = 16;
+constexpr int kProjCols = 16;
 constexpr int kProjKd = 4096;          // longest row
 constexpr int kProjChunks = kProjKd / 8 / 64;
 
 template <int MB>
 __global__ __launch_bounds__(kProjWaves * 64) void proj_few_kernel(const uint16_t* __restrict__ A, int M, ThinArgs s) {
-    using T = ThinI8<1>;
+    using T = ThinI8<1, false>;
     constexpr int P = 4;
+    static_assert(T::kCols == kProjCols, "a workgroup's columns");
     __shared__ __attribute__((aligned(16))) int8_t q[16 * MB * (kProjKd + 32) + T::kStep];
     __shared__ float scale[16 * MB];
     __shared__ f32x4 red[kProjWaves][64];
@@ -75,7 +77,7 @@ __global__ __launch_bounds__(kProjWaves * 64) void proj_few_kernel(const uint16_
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
                     a.v[b][h] = *(const u32x4*)&q[(16 * b + (lane & 15)) * stride + k + 64 * h + 16 * (lane >> 4)];
-            w[i].template mma<MB>(acc, a);
+            w[i].template mma<MB>(acc, a, nullptr);
             if (i0 + i + P < mine) w[i].load(rw, s, n0, k + kProjWaves * P * T::kStep, lane);
         }
     }
@@ -103,7 +105,7 @@ hipError_t launch_proj_few(const moe_bf16* A, const int8_t* W, const float* w_sc
                            moe_bf16* C, hipStream_t st) {
     if (M == 0) return hipSuccess;
     const ThinArgs s{nullptr, W, C, nullptr, w_scale, 0, (int64_t)N * Kd, 0, Kd, N, THIN_BF16};
-    const dim3 grid((unsigned)((N + ThinI8<1>::kCols - 1) / ThinI8<1>::kCols)), block(kProjWaves * 64);
+    const dim3 grid((unsigned)((N + kProjCols - 1) / kProjCols)), block(kProjWaves * 64);
     if (M <= 16) hipLaunchKernelGGL(proj_few_kernel<1>, grid, block, 0, st, A, (int)M, s);
     else hipLaunchKernelGGL(proj_few_kernel<2>, grid, block, 0, st, A, (int)M, s);
     return launch_check(st);
