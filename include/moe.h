@@ -611,7 +611,8 @@ int moe_grouped_gemm_i8(const int8_t* Aq, const float* a_scale, const void* sche
                         int32_t Kd, int32_t N, const int8_t* Wq, const float* w_scale, int32_t epilogue,
                         moe_bf16* C, hipStream_t stream);
 
-/* Workspace bytes moe_latent_proj_i8 needs; 0 for invalid sizes. */
+/* Workspace bytes moe_latent_proj_i8 needs; 0 for invalid sizes, which the call
+ * refuses, and for small calls (M <= 32, Kd <= 4096), whose ws may be NULL. */
 size_t moe_latent_proj_i8_workspace_bytes(int64_t M, int32_t Kd);
 
 /* moe_latent_proj with an 8-bit weight: the rows of A are quantised, then

@@ -384,9 +384,9 @@ def latent_proj_i8(A: torch.Tensor, Wq: torch.Tensor, w_scale: torch.Tensor):
     M, Kd = A.shape
     N = Wq.shape[0]
     _sizes(Wq.shape == (N, Kd) and w_scale.shape == (N,), "A, Wq and w_scale")
-    C = _empty((M, N), BF16, A.device)
-    ws = _ws(L.moe_latent_proj_i8_workspace_bytes(M, Kd), A.device)
-    L.moe_latent_proj_i8(A, Wq, w_scale, M, Kd, N, C, ws)
+    C = A.new_empty((M, N))
+    n = L.moe_latent_proj_i8_workspace_bytes(M, Kd)
+    L.moe_latent_proj_i8(A, Wq, w_scale, M, Kd, N, C, _ws(n, A.device) if n else None)
     return C
 
 
@@ -396,9 +396,8 @@ def grouped_ffn_i8(x_disp, offsets, W1q, s1, W2q, s2):
     E, F, _ = W1q.shape
     _sizes(W1q.shape == (E, F, D) and W2q.shape == (E, D, F) and s1.shape == (E, F) and s2.shape == (E, D)
            and offsets.shape == (E + 1,), "x_disp, offsets, weights and scales")
-    dev = x_disp.device
-    y_disp = _empty((R, D), BF16, dev)
-    ws = _ws(L.moe_grouped_ffn_i8_workspace_bytes(E, R, D, F), dev)
+    y_disp = x_disp.new_empty((R, D))
+    ws = _ws(L.moe_grouped_ffn_i8_workspace_bytes(E, R, D, F), x_disp.device)
     L.moe_grouped_ffn_i8(x_disp, offsets, E, R, D, F, W1q, s1, W2q, s2, y_disp, ws)
     return y_disp
 

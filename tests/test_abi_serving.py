@@ -48,12 +48,16 @@ def test_grouped_gemm_i8(lib):
 def test_latent_and_ffn_i8(lib):
     assert lib.moe_latent_proj_i8_workspace_bytes(5, 24) == 0
     assert lib.moe_latent_proj_i8_workspace_bytes(-1, 16) == 0
-    n = lib.moe_latent_proj_i8_workspace_bytes(5, 2688)
-    assert n >= 5 * 2688 + 20
+    assert lib.moe_latent_proj_i8_workspace_bytes(32, 4096) == 0    # a small call needs none
+    n = lib.moe_latent_proj_i8_workspace_bytes(33, 2688)
+    assert n >= 33 * 2688 + 33 * 4
+    assert lib.moe_latent_proj_i8_workspace_bytes(5, 4112) >= 5 * 4112 + 20
     f = lib.moe_latent_proj_i8
-    assert f(P, P, P, 5, 2688, 8, P, P, n - 1, None) == -4 and f(P, P, P, 5, 2688, 8, P, None, n, None) == -4
-    assert f(P, P, P, 5, 2688, 8, P, C.c_void_p(0x10010), n, None) == -3
-    assert f(P, P, P, 5, 2680, 8, P, P, n, None) == -2 and f(P, P, None, 5, 2688, 8, P, P, n, None) == -1
+    assert f(P, P, P, 33, 2688, 8, P, P, n - 1, None) == -4 and f(P, P, P, 33, 2688, 8, P, None, n, None) == -4
+    assert f(P, P, P, 33, 2688, 8, P, C.c_void_p(0x10010), n, None) == -3
+    assert f(P, P, P, 33, 2680, 8, P, P, n, None) == -2 and f(P, P, None, 33, 2688, 8, P, P, n, None) == -1
+    assert f(P, P, P, 5, 2680, 8, P, None, 0, None) == -2 and f(P, P, P, -1, 2688, 8, P, None, 0, None) == -2
+    assert f(ODD, P, P, 5, 2688, 8, P, None, 0, None) == -3 and f(P, P, P, 0, 2688, 8, P, None, 0, None) == 0
     g = lib.moe_grouped_ffn_i8
     n = lib.moe_grouped_ffn_i8_workspace_bytes(8, 1000, 64, 48)
     assert n >= 1000 * (64 + 2 * 48)
