@@ -920,7 +920,7 @@ int moe_grouped_gemm_i8(const int8_t* Aq, const float* a_scale, const void* sche
 }
 
 size_t moe_latent_proj_i8_workspace_bytes(int64_t M, int32_t Kd) {
-    if (M < 0 || M >= kMaxRows || !dim16_ok(Kd) || moe::proj_few_fits(M, Kd)) return 0;
+    if (M < 0 || M >= kMaxRows || !dim16_ok(Kd) || (M <= moe::kProjFewRows && Kd <= moe::kProjKd)) return 0;
     return align256((size_t)M * Kd) + align256((size_t)M * 4);
 }
 
@@ -932,9 +932,10 @@ int moe_latent_proj_i8(const moe_bf16* A, const int8_t* Wq, const float* w_scale
     MOE_TRY(need(Wq, (uint64_t)Kd * N, 16));
     MOE_TRY(need(w_scale, (uint64_t)N * 4, 16));
     MOE_TRY(need(C, (uint64_t)M * N * 2, 16));
-    if (moe::proj_few_fits(M, Kd)) return hip_status(moe::launch_proj_few(A, Wq, w_scale, M, N, Kd, C, stream));
-    if (ws == nullptr || ws_bytes < moe_latent_proj_i8_workspace_bytes(M, Kd)) return MOE_ERR_WORKSPACE;
+    const size_t wsn = moe_latent_proj_i8_workspace_bytes(M, Kd);
+    if (wsn > 0 && (ws == nullptr || ws_bytes < wsn)) return MOE_ERR_WORKSPACE;
     MOE_TRY(opt(ws, 256));
+    if (moe::proj_few_fits(M, N, Kd)) return hip_status(moe::launch_proj_few(A, Wq, w_scale, M, N, Kd, C, stream));
     int8_t* q = (int8_t*)ws;
     float* scale = (float*)((char*)ws + align256((size_t)M * Kd));
     MOE_HIP(moe::launch_quant_rows(A, M, Kd, q, scale, stream));

@@ -116,8 +116,11 @@ hipError_t launch_grouped_rows_mx(const uint8_t* Aq, const uint8_t* A_scale, con
 hipError_t launch_grouped_rows_i8(const int8_t* A, const float* a_scale, const int8_t* B, const float* b_scale,
                                   void* C, bool relu2, const void* sched, int E, int64_t R, int N, int Kd,
                                   hipStream_t st);
-// C = bf16 of A's rows, quantised, times W [N, Kd] (E = 1 above) for the M and Kd that proj_few_fits, in one launch (thin.hip).
-bool proj_few_fits(int64_t M, int Kd);
+// C = bf16 of A's rows, quantised, times W [N, Kd] (E = 1 above) for sizes that proj_few_fits, in one launch (thin.hip): up to
+// kProjFewRows rows whatever N, and more while they are one round of workgroups.
+constexpr int kProjFewRows = 32;
+constexpr int kProjKd = 4096;   // longest row
+bool proj_few_fits(int64_t M, int N, int Kd);
 hipError_t launch_proj_few(const moe_bf16* A, const int8_t* W, const float* w_scale, int64_t M, int N, int Kd,
                            moe_bf16* C, hipStream_t st);
 // 8-bit rows: scale[r] = max|x[r, :]| / 127 and the codes of x[r, :] (quant.hip).  With sched (and offsets

@@ -1,9 +1,10 @@
-// The 8-bit dense product of at most 32 bf16 rows in one launch (thin.h), their
-// quantisation included.  Such a call is latency: of its launches, and of one pass over
-// the rows and one over the weights.  So every workgroup quantises all rows for itself
-// into LDS (a wave a row) while its 16 columns' weights are on their way, and its 16 waves
-// share the contraction.  5 x 2,688 x 672: 18.8 us as a launch each for the
-// codes and the 128-row tiles, 5.0 as this.
+// The 8-bit dense product of few bf16 rows in one launch (thin.h), their quantisation
+// included.  Such a call is latency: of its launches, and of one pass over the rows and one
+// over the weights.  So every workgroup quantises its 16 or 32 rows for itself into LDS (a
+// wave a row at a time) while its 16 columns' weights are on their way, and its 16 waves share
+// the contraction.  Measured, this / a launch each for the codes and the tiles of
+// gemm.hip: 2,688 x 672 1 row 5.3 / 17.4 us, 16 6.9 / 17.5, 32 10.4 / 17.6, 192 11.2 / 18.0; 4,096 x
+// 1,024 1 row 6.0 / 23.5, 128 13.3 / 23.8; 512 x 512 256 rows 7.6 / 8.9.
 #include "kernels.h"
 #include "quant8.h"
 #include "thin.h"
@@ -12,7 +13,6 @@ namespace moe {
 
 constexpr int kProjWaves = 16;
 constexpr int kProjCols = 16;
-constexpr int kProjKd = 4096;          // longest row
 constexpr int kProjChunks = kProjKd / 8 / 64;
 
 template <int MB>
@@ -25,6 +25,9 @@ __global__ __launch_bounds__(kProjWaves * 64) void proj_few_kernel(const uint16_
     __shared__ f32x4 red[kProjWaves][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n0 = blockIdx.x * T::kCols;
+    A += (int64_t)blockIdx.y * 16 * MB * s.Kd;
+    s.out = (uint16_t*)s.out + (int64_t)blockIdx.y * 16 * MB * s.N;
+    M -= blockIdx.y * 16 * MB;   // rows from this workgroup's first on
     const int nst = (s.Kd + T::kStep - 1) / T::kStep;
     const int mine = nst > wave ? (nst - wave + kProjWaves - 1) / kProjWaves : 0;
     const __amdgpu_buffer_rsrc_t rw = thin_rsrc(s.W, s.w_bytes);
@@ -99,15 +102,19 @@ __global__ __launch_bounds__(kProjWaves * 64) void proj_few_kernel(const uint16_
     }
 }
 
-bool proj_few_fits(int64_t M, int Kd) { return M <= 32 && Kd <= kProjKd; }
+// One round of workgroups, each of which fills a CU's LDS.
+bool proj_few_fits(int64_t M, int N, int Kd) {
+    return Kd <= kProjKd && (M <= kProjFewRows || (M + 31) / 32 * ((N + kProjCols - 1) / kProjCols) <= cu_count());
+}
 
 hipError_t launch_proj_few(const moe_bf16* A, const int8_t* W, const float* w_scale, int64_t M, int N, int Kd,
                            moe_bf16* C, hipStream_t st) {
     if (M == 0) return hipSuccess;
     const ThinArgs s{nullptr, W, C, nullptr, w_scale, 0, (int64_t)N * Kd, 0, Kd, N, THIN_BF16};
-    const dim3 grid((unsigned)((N + kProjCols - 1) / kProjCols)), block(kProjWaves * 64);
-    if (M <= 16) hipLaunchKernelGGL(proj_few_kernel<1>, grid, block, 0, st, A, (int)M, s);
-    else hipLaunchKernelGGL(proj_few_kernel<2>, grid, block, 0, st, A, (int)M, s);
+    const unsigned nx = (unsigned)((N + kProjCols - 1) / kProjCols);
+    const dim3 block(kProjWaves * 64);
+    if (M <= 16) hipLaunchKernelGGL(proj_few_kernel<1>, dim3(nx), block, 0, st, A, (int)M, s);
+    else hipLaunchKernelGGL(proj_few_kernel<2>, dim3(nx, (unsigned)((M + 31) / 32)), block, 0, st, A, (int)M, s);
     return launch_check(st);
 }
 
