@@ -70,6 +70,12 @@ __global__ __launch_bounds__(kFewThreads) void few_logits_kernel(const uint16_t*
             (red[0][t][lane] + red[1][t][lane]) + (red[2][t][lane] + red[3][t][lane]);
 }
 
+// What the lanes of a wave wrote to LDS before is what they read after.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 __device__ __forceinline__ uint32_t wave_max_code(uint32_t v) {
     v = row_max_u32(v);
     const uint32_t a = __builtin_amdgcn_readlane(v, 0), b = __builtin_amdgcn_readlane(v, 16);
@@ -96,6 +102,7 @@ __device__ __forceinline__ void few_pick(const uint32_t (&code)[EPL], uint32_t t
     }
     if constexpr (EPL == 1) {   // the lanes' ranks themselves
         if (before < K) cand[before] = make_uint2(top, (uint32_t)lane);
+        wave_sync();
         if (lane < K) {
             const uint2 mine = cand[lane];
             my_c = mine.x;
@@ -135,14 +142,17 @@ __device__ __forceinline__ void few_pick(const uint32_t (&code)[EPL], uint32_t t
         }
         return;
     }
-    // larger code first, then the lower expert; the lanes of one wave write and read cand in order
+    // larger code first, then the lower expert
+    wave_sync();
     const uint2 c = lane < n ? cand[lane] : make_uint2(0u, 1023u);
     int rank = 0;
     for (int j = 0; j < n; ++j) {
         const uint32_t oc = __builtin_amdgcn_readlane(c.x, j), oe = __builtin_amdgcn_readlane(c.y, j);
         rank += oc > c.x || (oc == c.x && oe < c.y) ? 1 : 0;
     }
+    wave_sync();   // every lane has its candidate
     if (lane < n && rank < K) cand[rank] = c;
+    wave_sync();
     if (lane < K) {
         const uint2 mine = cand[lane];
         my_c = mine.x;
@@ -256,12 +266,13 @@ struct FewGemmArgs {
     int epi;
 };
 
-// The a-th expert (ascending) among the n picks and its rows, in order, in rows[];
+// The a-th expert (ascending) among at most kFewSearch picks and its rows, in order, in rows[];
 // returns the expert, or -1 if fewer are picked.  A single token's picks are distinct and
 // need no order.  Every thread of the workgroup calls it.
+constexpr int kFewSearch = 256;   // most picks that a workgroup searches
 struct FewPicks {
     uint32_t seen[32];
-    int32_t picks[kFewMaxTokens * 32], rows[kFewMaxTokens], nrows;
+    int32_t picks[kFewSearch], rows[kFewMaxTokens], nrows;
 };
 __device__ __forceinline__ int few_plan(const int32_t* __restrict__ idx, int S, int K, int a, FewPicks& sh) {
     const int tid = threadIdx.x, lane = tid & 63, n = S * K;
@@ -506,7 +517,7 @@ int few_share(bool i8, bool many, int slabs, int steps) {
 // workgroup of both products.  64 tokens top-22 of 512 422 us against 459 and, in 8 bits, 251
 // against 330; 40 tokens top-22 of 64 51 / 54; 64 tokens top-6 of 64 (384 picks) 121 / 121; 16 tokens
 // top-8 of 256 (128 picks) 349 / 348.
-bool few_table_pays(int picks) { return picks > 256; }
+bool few_table_pays(int picks) { return picks > kFewSearch; }
 
 // Columns of a slab.  8-bit weights take 32, or, where more than 16 tokens give an expert
 // several rows, 64, which halves how often they are read (us with 32 / 64: 64 tokens top-6 of

@@ -138,7 +138,7 @@ struct ThinI8 {
         const int lane = threadIdx.x & 63;
         u32x4 f[NB][2];
         if constexpr (NT) {
-            // a wave's LDS operations are in order: no barrier between its writes and reads
+            // a wave's LDS operations are done in order: the fences keep the compiler to it
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -146,6 +146,7 @@ struct ThinI8 {
                     const int r = 8 * h + (lane >> 3);
                     *(u32x4*)(stage + b * 2048 + r * 128 + (((lane & 7) ^ rswz(r)) * 16)) = w[b][h];
                 }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
             for (int b = 0; b < NB; ++b)
@@ -154,6 +155,7 @@ struct ThinI8 {
                     const int r = lane & 15, c = 4 * h + (lane >> 4);
                     f[b][h] = *(const u32x4*)(stage + b * 2048 + r * 128 + ((c ^ rswz(r)) * 16));
                 }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
         } else {
 #pragma unroll

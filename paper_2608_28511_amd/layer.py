@@ -409,8 +409,8 @@ class LayerFew:
     channel scales s1 and s2 given, int8 as quant_weights_i8 returns them; the shared
     expert's (Ws1, Ws2, with ss1 and ss2) likewise.  A call takes x [n, D] of any
     n <= S tokens and returns y [n, D], topk_idx and topk_prob [n, K], which the next call
-    overwrites.  Calls of one object share its workspace: on several streams, or
-    replayed from several graphs, they must be ordered; objects are independent.
+    overwrites.  Calls of one object share its workspace: from several threads, on several
+    streams, or replayed from several graphs, they must be ordered; objects are independent.
     """
 
     def __init__(self, S, Wr, W1, W2, K, bias=None, sel_bias=None, score="softmax", s1=None, s2=None, Ws1=None,
@@ -450,6 +450,8 @@ class LayerFew:
     def __call__(self, x: torch.Tensor) -> Dict[str, torch.Tensor]:
         n, D = x.shape
         _sizes(D == self.D and n <= self.S, "x")
+        if x.device != self.ws.device:
+            raise ValueError(f"x is on {x.device}, the layer on {self.ws.device}")
         a = self._args
         a.S = n
         a.x = L._here(x, BF16, "x")

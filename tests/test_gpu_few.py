@@ -153,6 +153,26 @@ def test_sizes_of_bf16_alone(D, F):
     check_bf16(m, x, m.layer(9)(x))
 
 
+@pytest.mark.parametrize("S", [12, 20])
+@pytest.mark.parametrize("weights, D, F", [("bf16", 2048, 1024), ("bf16", 1040, 2048), ("i8", 2048, 1024),
+                                           ("i8", 1040, 2048)])
+def test_weights_past_the_last_level_cache(weights, D, F, S):
+    """Weights over 256 MB are read another way, where their rows start on cache lines."""
+    m = Model(D, 80, 8, F, seed=11, weights=weights)
+    x = m.tokens(S)
+    (check_i8 if weights == "i8" else check_bf16)(m, x, m.layer(S)(x))
+    if D == 2048:   # the same weights off the cache lines: the same sums
+        ref = {k: v.clone() for k, v in m.layer(S)(x).items()}
+        for name in ("w1", "w2"):
+            w = getattr(m, name)
+            buf = torch.empty(w.numel() + 64, dtype=w.dtype, device=DEV)
+            off = 16 // w.element_size()
+            buf[off:off + w.numel()] = w.reshape(-1)
+            setattr(m, name, buf[off:off + w.numel()].view(w.shape))
+        for k, v in m.layer(S)(x).items():
+            assert torch.equal(v, ref[k]), k
+
+
 @pytest.mark.parametrize("weights", ["bf16", "i8"])
 def test_fewer_tokens_than_the_layer_holds(weights):
     m = Model(144, 12, 3, 176, 64, "sigmoid", weights, seed=3)
