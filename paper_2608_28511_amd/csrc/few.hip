@@ -373,9 +373,11 @@ __global__ __launch_bounds__(kTableThreads) void few_table_kernel(const int32_t*
     }
 }
 
-// MBMAX = 1: at most 16 tokens, so at most 16 rows an expert; four waves a SIMD.
+// At most 16 MBMAX tokens, and so rows an expert.  The fewer, the more waves a SIMD has registers for: 32
+// tokens of 8-bit weights top-16 of 256 122 us at four, 142 at the two that 64 leave; bf16 weights 215 / 217.
+constexpr int few_waves(int mb_max, int wave_lds) { return mb_max == 4 ? 2 : wave_lds * mb_max <= 8192 ? 4 : 3; }
 template <class T, int MBMAX>
-__global__ __launch_bounds__(kFewThreads, MBMAX == 1 ? 4 : 2) void few_gemm_kernel(FewGemmArgs p) {
+__global__ __launch_bounds__(kFewThreads, few_waves(MBMAX, T::kWaveLds)) void few_gemm_kernel(FewGemmArgs p) {
     __shared__ FewPicks sh;
     __shared__ __attribute__((aligned(16))) char lds[4 * T::kWaveLds];
     const bool shared = (int)blockIdx.x >= p.r_items;
@@ -622,6 +624,8 @@ hipError_t launch_layer_few(const moe_layer_few_args* a, hipStream_t st) {
             constexpr bool NT = decltype(nt)::value;
             if (S <= 16) i8 ? go(few_gemm_kernel<ThinI8<2, NT>, 1>) : go(few_gemm_kernel<ThinBf16<NT>, 1>);
             else if (!i8) go(few_gemm_kernel<ThinBf16<NT>, 4>);
+            else if (S <= 32)
+                cols == kSlabI8 ? go(few_gemm_kernel<ThinI8<2, NT>, 2>) : go(few_gemm_kernel<ThinI8<4, NT>, 2>);
             else cols == kSlabI8 ? go(few_gemm_kernel<ThinI8<2, NT>, 4>) : go(few_gemm_kernel<ThinI8<4, NT>, 4>);
         };
         if (thin_nt(r.W, (int64_t)(i8 ? r.Kd : r.N) * wb, 2 * (int64_t)p.r_experts * r.w_bytes)) pick(std::true_type{});
