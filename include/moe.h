@@ -668,8 +668,8 @@ typedef struct {
     size_t ws_bytes;
 } moe_layer_few_args;
 
-/* Workspace bytes for these sizes and modes (no pointer is read); 0 if they are
- * invalid or S = 0. */
+/* Workspace bytes for these sizes and modes (no pointer is read), enough for any
+ * smaller S too; 0 if they are invalid or S = 0. */
 size_t moe_layer_few_workspace_bytes(const moe_layer_few_args* a);
 
 /* y[t] = bf16( sum_k p[t,k] FFN_{T_k}(x[t]) [+ shared(x[t])] ): moe_layer_fwd's

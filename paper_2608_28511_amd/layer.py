@@ -409,7 +409,7 @@ class LayerFew:
     channel scales s1 and s2 given, int8 as quant_weights_i8 returns them; the shared
     expert's (Ws1, Ws2, with ss1 and ss2) likewise.  A call takes x [n, D] of any
     n <= S tokens and returns y [n, D], topk_idx and topk_prob [n, K], which the next call
-    overwrites.  Calls of one object share its workspace: from several threads, on several
+    overwrites (its x may be that y).  Calls of one object share its workspace: from several threads, on several
     streams, or replayed from several graphs, they must be ordered; objects are independent.
     """
 
@@ -437,14 +437,10 @@ class LayerFew:
             S, D, E, K, F, Fs, {"softmax": L.SCORE_SOFTMAX, "sigmoid": L.SCORE_SIGMOID}[score],
             L.WEIGHTS_I8 if i8 else L.WEIGHTS_BF16, Wr=Wr, router_bias=bias, sel_bias=sel_bias, W1=W1, W2=W2, Ws1=Ws1,
             Ws2=Ws2, s1=s1, s2=s2, ss1=ss1, ss2=ss2, **self.out)
-        # a smaller call may share its contractions among more workgroups, whose sums take more room
-        sizes = []
-        for n in range(1, S + 1):
-            self._args.S = n
-            sizes.append(L.moe_layer_few_workspace_bytes(self._args))
-        if S > 0 and min(sizes) == 0:
+        n = L.moe_layer_few_workspace_bytes(self._args)
+        if S > 0 and n == 0:
             raise ValueError("invalid layer shape")
-        self.ws = _ws(max(sizes, default=1), dev)
+        self.ws = _ws(n or 1, dev)
         self._args.ws, self._args.ws_bytes = self.ws.data_ptr(), self.ws.numel()
 
     def __call__(self, x: torch.Tensor) -> Dict[str, torch.Tensor]:

@@ -102,6 +102,14 @@ def test_layer_few_workspace(lib):
     assert lib.moe_layer_few(C.byref(_few(ws_bytes=n - 1)), None) == -4
 
 
+@pytest.mark.parametrize("weights", [0, 1])
+@pytest.mark.parametrize("sizes", [dict(D=32, E=8, K=2, F=48), dict(D=2688, E=512, K=22, F=1344, Fs=2688),
+                                   dict(D=4096, E=64, K=32, F=16)])
+def test_layer_few_workspace_serves_fewer_tokens(lib, sizes, weights):
+    n = [lib.moe_layer_few_workspace_bytes(C.byref(_few(S=S, weights=weights, **sizes))) for S in range(1, 65)]
+    assert n == sorted(n) and n[0] > 0
+
+
 def test_few_struct_layout(tmp_path):
     """The ctypes mirror has the C layout (offsets printed by a C program)."""
     import shutil

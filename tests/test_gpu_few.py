@@ -173,6 +173,56 @@ def test_weights_past_the_last_level_cache(weights, D, F, S):
             assert torch.equal(v, ref[k]), k
 
 
+@pytest.mark.parametrize("S", [32, 48])
+def test_wide_slabs_past_the_last_level_cache(S):
+    """8-bit weights over 256 MB, and several rows an expert."""
+    m = Model(2048, 80, 10, 1024, seed=12, weights="i8")
+    x = m.tokens(S)
+    check_i8(m, x, m.layer(S)(x))
+
+
+@pytest.mark.parametrize("weights", ["bf16", "i8"])
+def test_experts_past_4_gib(weights):
+    """The last experts of a large layer give what they give as a small layer's."""
+    D, F, E = 2048, 2080, 1024 if weights == "i8" else 520
+    i8 = weights == "i8"
+    g = torch.Generator(device=DEV).manual_seed(13)
+    few = 4
+    shapes = [(F, D), (D, F)] if i8 else [(D, F), (F, D)]
+    small = [torch.randint(-127, 128, (few,) + s, generator=g, device=DEV).to(torch.int8 if i8 else BF16)
+             for s in shapes]
+    large = [torch.zeros((E,) + s, dtype=small[0].dtype, device=DEV) for s in shapes]
+    for a, b in zip(large, small):
+        a[-few:] = b
+    past = (E - few) * F * D * large[0].element_size() > 2 ** 32
+    assert past
+    x = torch.randn((2, D), generator=g, device=DEV).to(BF16)
+    sc = torch.rand((few, D), generator=g, device=DEV) if i8 else None
+
+    def run(W, E):
+        bias = torch.full((E,), float("-inf"), device=DEV)
+        bias[-few:] = torch.arange(few, device=DEV).float()
+        kw = dict(s1=torch.ones((E, F), device=DEV), s2=torch.zeros((E, D), device=DEV)) if i8 else {}
+        if i8:
+            kw["s2"][-few:] = sc
+        return layer.LayerFew(2, torch.zeros((D, E), device=DEV), *W, 2, bias=bias, **kw)(x)
+
+    a, b = run(large, E), run(small, few)
+    assert torch.equal(a["topk_idx"], b["topk_idx"] + (E - few)) and torch.equal(a["topk_prob"], b["topk_prob"])
+    assert torch.equal(a["y"], b["y"]) and bool((a["y"] != 0).any())
+
+
+@pytest.mark.parametrize("weights", ["bf16", "i8"])
+def test_a_layer_fed_with_its_own_output(weights):
+    m = Model(272, 12, 3, 176, 64, weights=weights, seed=14)
+    lf = m.layer(5)
+    x = m.tokens(5)
+    once = lf(x)["y"].clone()
+    ref = {k: v.clone() for k, v in lf(once).items()}
+    for k, v in lf(lf(x)["y"]).items():
+        assert torch.equal(v, ref[k]), k
+
+
 @pytest.mark.parametrize("weights", ["bf16", "i8"])
 def test_fewer_tokens_than_the_layer_holds(weights):
     m = Model(144, 12, 3, 176, 64, "sigmoid", weights, seed=3)

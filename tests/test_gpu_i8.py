@@ -219,6 +219,29 @@ def test_grouped_ffn_i8_exact_hidden():
     assert np.array_equal(round_bf16(np64(y)), np64(y))
 
 
+def test_rows_past_4_gib():
+    """The last rows of a call give what they give alone."""
+    R, D, N = 530_003, 8192, 16
+    g = torch.Generator(device=DEV).manual_seed(21)
+    tail = torch.randn((300, D), generator=g, device=DEV).to(BF16)
+    x = torch.zeros((R, D), dtype=BF16, device=DEV)
+    x[-300:] = tail
+    q, scale = layer.quant_rows_i8(x)
+    qt, st = layer.quant_rows_i8(tail)
+    past = q.numel() > 2 ** 32
+    assert past and torch.equal(q[-300:], qt) and torch.equal(scale[-300:], st)
+    assert not bool(scale[:-300].any())
+    W = torch.randn((2, D, N), generator=g, device=DEV).to(BF16)
+    Wq, ws = layer.quant_weights_i8(W)
+    off = torch.tensor([0, R - 150, R], dtype=torch.int32, device=DEV)
+    y = layer.grouped_gemm_i8(q, scale, layer.grouped_schedule(off, 2, R), Wq, ws, 0)
+    for e, part in ((0, slice(0, 150)), (1, slice(150, 300))):
+        ref = layer.grouped_gemm_i8(qt[part].contiguous(), st[part].contiguous(), None, Wq[e:e + 1], ws[e:e + 1], 0)
+        assert torch.equal(y[R - 300:][part], ref)
+    assert not bool(y[:-300].any())
+    assert torch.equal(layer.latent_proj_i8(x, Wq[0], ws[0])[-300:], layer.latent_proj_i8(tail, Wq[0], ws[0]))
+
+
 def test_rows_that_are_not_finite_stay_alone():
     x, off, W1q, s1, W2q, s2 = ffn_inputs([100, 0, 57], 64, 128, 6)
     clean = layer.grouped_ffn_i8(x, off, W1q, s1, W2q, s2)
