@@ -116,8 +116,8 @@ hipError_t launch_grouped_rows_mx(const uint8_t* Aq, const uint8_t* A_scale, con
 hipError_t launch_grouped_rows_i8(const int8_t* A, const float* a_scale, const int8_t* B, const float* b_scale,
                                   void* C, bool relu2, const void* sched, int E, int64_t R, int N, int Kd,
                                   hipStream_t st);
-// C = bf16 of A's rows, quantised, times W [N, Kd] (E = 1 above) for sizes that proj_few_fits, in one launch (thin.hip): up to
-// kProjFewRows rows whatever N, and more while they are one round of workgroups.
+// C = bf16 of A's rows, quantised, times W [N, Kd] (E = 1 above) for sizes that proj_few_fits, in one launch
+// (thin.hip): up to kProjFewRows rows whatever N, and more while they are one round of workgroups.
 constexpr int kProjFewRows = 32;
 constexpr int kProjKd = 4096;   // longest row
 bool proj_few_fits(int64_t M, int N, int Kd);
