@@ -1,10 +1,11 @@
 // The 8-bit dense product of few bf16 rows in one launch (thin.h), their quantisation
 // included.  Such a call is latency: of its launches, and of one pass over the rows and one
 // over the weights.  So every workgroup quantises its 16 or 32 rows for itself into LDS (a
-// wave a row at a time) while its 16 columns' weights are on their way, and its 16 waves share
-// the contraction.  Measured, this / a launch each for the codes and the tiles of
-// gemm.hip: 2,688 x 672 1 row 5.3 / 17.4 us, 16 6.9 / 17.5, 32 10.4 / 17.6, 192 11.2 / 18.0; 4,096 x
-// 1,024 1 row 6.0 / 23.5, 128 13.3 / 23.8; 512 x 512 256 rows 7.6 / 8.9.
+// wave a row at a time) while its first columns' weights are on their way, and its 16 waves share
+// the contraction of one slab of columns, or of two.  Measured, this / a launch each for the codes
+// and the tiles of gemm.hip: 2,688 x 672 1 row 5.2 / 17.4 us, 32 10.3 / 17.5, 192 11.3 / 18.0, 256 12.2 /
+// 18.0, 700 15.1 / 18.4; 4,096 x 1,024 1 row 6.0 / 22.7, 128 13.3 / 24.0, 512 18.9 / 24.6; 512 x 512
+// 256 rows 7.6 / 8.9, 1,024 8.3 / 9.0.
 #include "kernels.h"
 #include "quant8.h"
 #include "thin.h"
@@ -12,29 +13,31 @@
 namespace moe {
 
 constexpr int kProjWaves = 16;
-constexpr int kProjCols = 16;
 constexpr int kProjChunks = kProjKd / 8 / 64;
 
-template <int MB>
+// 16 MB rows and 16 / WK slabs of 16 NB columns a workgroup; WK waves share a slab.
+template <int MB, int NB, int WK>
 __global__ __launch_bounds__(kProjWaves * 64) void proj_few_kernel(const uint16_t* __restrict__ A, int M, ThinArgs s) {
-    using T = ThinI8<1, false>;
-    constexpr int P = 4;
-    static_assert(T::kCols == kProjCols, "a workgroup's columns");
-    __shared__ __attribute__((aligned(16))) int8_t q[16 * MB * (kProjKd + 32) + T::kStep];
+    using T = ThinI8<NB, false>;
+    constexpr int P = 4 / NB, kPieces = MB * NB;   // steps ahead; 16 x 16 tiles of a slab
+    constexpr int kCodes = 16 * MB * (kProjKd + 32) + T::kStep, kSums = kProjWaves * kPieces * 1024;
+    constexpr bool kApart = kCodes + kSums < 160 * 1024 - 256;   // the waves' sums have LDS of their own
+    static_assert(kSums <= kCodes, "sums take the codes' place");
+    __shared__ __attribute__((aligned(16))) int8_t q[kCodes + (kApart ? kSums : 0)];
     __shared__ float scale[16 * MB];
-    __shared__ f32x4 red[kProjWaves][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n0 = blockIdx.x * T::kCols;
+    const int slab = wave / WK, kk = wave % WK;
+    const int n0 = ((int)blockIdx.x * (kProjWaves / WK) + slab) * T::kCols;
     A += (int64_t)blockIdx.y * 16 * MB * s.Kd;
     s.out = (uint16_t*)s.out + (int64_t)blockIdx.y * 16 * MB * s.N;
     M -= blockIdx.y * 16 * MB;   // rows from this workgroup's first on
     const int nst = (s.Kd + T::kStep - 1) / T::kStep;
-    const int mine = nst > wave ? (nst - wave + kProjWaves - 1) / kProjWaves : 0;
+    const int mine = n0 < s.N && nst > kk ? (nst - kk + WK - 1) / WK : 0;
     const __amdgpu_buffer_rsrc_t rw = thin_rsrc(s.W, s.w_bytes);
     T w[P];
 #pragma unroll
     for (int i = 0; i < P; ++i)
-        if (i < mine) w[i].load(rw, s, n0, (wave + kProjWaves * i) * T::kStep, lane);
+        if (i < mine) w[i].load(rw, s, n0, (kk + WK * i) * T::kStep, lane);
 
     // rows an odd number of 16-byte chunks apart: the fragment reads of 16 rows spread over the banks
     const int stride = s.Kd + ((s.Kd / 16) & 1 ? 32 : 16);
@@ -59,41 +62,44 @@ __global__ __launch_bounds__(kProjWaves * 64) void proj_few_kernel(const uint16_
 #pragma unroll
         for (int i = 0; i < kProjChunks; ++i) {
             const int c = lane + 64 * i;
-            if (c < n) *(uint2*)&q[r * stride + c * 8] = make_uint2(codes4(z, v[i].x, v[i].y), codes4(z, v[i].z, v[i].w));
+            if (c < n)
+                *(uint2*)&q[r * stride + c * 8] = make_uint2(codes4(z, v[i].x, v[i].y), codes4(z, v[i].z, v[i].w));
         }
     }
     __syncthreads();
 
     // Rows past M and codes past Kd read what LDS holds there: the former leave no
     // result, the latter meet zero weights.
-    f32x4 acc[MB][1];
+    f32x4 acc[MB][NB];
 #pragma unroll
-    for (int b = 0; b < MB; ++b) acc[b][0] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int v = 0; v < kPieces; ++v) acc[v / NB][v % NB] = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int i0 = 0; i0 < mine; i0 += P) {
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             if (i0 + i >= mine) break;
-            const int k = (wave + kProjWaves * (i0 + i)) * T::kStep;
-            T::A<MB> a;
+            const int k = (kk + WK * (i0 + i)) * T::kStep;
+            typename T::template A<MB> a;
 #pragma unroll
             for (int b = 0; b < MB; ++b)
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
                     a.v[b][h] = *(const u32x4*)&q[(16 * b + (lane & 15)) * stride + k + 64 * h + 16 * (lane >> 4)];
             w[i].template mma<MB>(acc, a, nullptr);
-            if (i0 + i + P < mine) w[i].load(rw, s, n0, k + kProjWaves * P * T::kStep, lane);
+            if (i0 + i + P < mine) w[i].load(rw, s, n0, k + WK * P * T::kStep, lane);
         }
     }
+    if constexpr (!kApart) __syncthreads();   // the codes are read: the waves' sums take their place
+    f32x4* const sums = (f32x4*)(q + (kApart ? kCodes : 0));
+    auto sum = [&](int of, int v) -> f32x4& { return sums[(of * kPieces + v) * 64 + lane]; };
 #pragma unroll
-    for (int b = 0; b < MB; ++b) {
-        if (b > 0) __syncthreads();
-        red[wave][lane] = acc[b][0];
-        __syncthreads();
-        const int r = 16 * b + (lane & 15), col = n0 + T::piece_col(0, lane);
-        if (wave != 0 || r >= M || col >= s.N) continue;   // N is a multiple of 8
-        f32x4 t = red[0][lane];
+    for (int v = 0; v < kPieces; ++v) sum(wave, v) = acc[v / NB][v % NB];
+    __syncthreads();
+        for (int v = kk; v < kPieces; v += WK) {
+        const int r = 16 * (v / NB) + (lane & 15), col = n0 + T::piece_col(v % NB, lane);
+        if (r >= M || col >= s.N) continue;   // N is a multiple of 8
+        f32x4 t = sum(slab * WK, v);
 #pragma unroll
-        for (int j = 1; j < kProjWaves; ++j) t = thin_add<true>(t, red[j][lane]);
+        for (int j = 1; j < WK; ++j) t = thin_add<true>(t, sum(slab * WK + j, v));
         const f32x4 cs = *(const f32x4*)(s.col_scale + col);
 #pragma unroll
         for (int u = 0; u < 4; ++u) t[u] = (float)__float_as_int(t[u]) * scale[r] * cs[u];
@@ -102,19 +108,34 @@ __global__ __launch_bounds__(kProjWaves * 64) void proj_few_kernel(const uint16_
     }
 }
 
-// One round of workgroups, each of which fills a CU's LDS.
-bool proj_few_fits(int64_t M, int N, int Kd) {
-    return Kd <= kProjKd && (M <= kProjFewRows || (M + 31) / 32 * ((N + kProjCols - 1) / kProjCols) <= cu_count());
+namespace {
+
+// Columns of a workgroup that still make one round of workgroups, each of which fills a CU's LDS: 16,
+// 32 or 64; 0 if those do not suffice.  The fewest (us with 16 / 32: 128 rows of 2,688 x 672 10.9 / 11.7, of
+// 4,096 x 1,024 13.2 / 14.1).  More lose to the two launches (1,024 rows at 128 columns: 2,688 x 672
+// 19.6 / 18.8, 4,096 x 1,024 28.2 / 26.0), and so do more than 16 of a short contraction, whose two
+// launches are latency alone (256 rows of 48 x 1,000 8.5 / 7.7).
+int proj_cols(int64_t M, int N, int Kd) {
+    for (int cols = 16; cols <= (Kd < 256 ? 16 : 64); cols *= 2)
+        if ((M + 31) / 32 * ((N + cols - 1) / cols) <= cu_count()) return cols;
+    return M <= kProjFewRows ? 16 : 0;
 }
+
+}  // namespace
+
+bool proj_few_fits(int64_t M, int N, int Kd) { return Kd <= kProjKd && proj_cols(M, N, Kd) > 0; }
 
 hipError_t launch_proj_few(const moe_bf16* A, const int8_t* W, const float* w_scale, int64_t M, int N, int Kd,
                            moe_bf16* C, hipStream_t st) {
     if (M == 0) return hipSuccess;
     const ThinArgs s{nullptr, W, C, nullptr, w_scale, 0, (int64_t)N * Kd, 0, Kd, N, THIN_BF16};
-    const unsigned nx = (unsigned)((N + kProjCols - 1) / kProjCols);
-    const dim3 block(kProjWaves * 64);
-    if (M <= 16) hipLaunchKernelGGL(proj_few_kernel<1>, dim3(nx), block, 0, st, A, (int)M, s);
-    else hipLaunchKernelGGL(proj_few_kernel<2>, dim3(nx, (unsigned)((M + 31) / 32)), block, 0, st, A, (int)M, s);
+    const int cols = M <= 16 ? 16 : proj_cols(M, N, Kd);
+    const dim3 block(kProjWaves * 64), grid((unsigned)((N + cols - 1) / cols), (unsigned)((M + 31) / 32));
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, A, (int)M, s); };
+    if (M <= 16) go(proj_few_kernel<1, 1, 16>);
+    else if (cols == 16) go(proj_few_kernel<2, 1, 16>);
+    else if (cols == 32) go(proj_few_kernel<2, 2, 16>);
+    else go(proj_few_kernel<2, 2, 8>);
     return launch_check(st);
 }
 

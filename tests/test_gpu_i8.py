@@ -159,6 +159,14 @@ def test_latent_proj_i8(M, Kd, N):
     assert torch.equal(layer.grouped_gemm_i8(q, sx, None, Wq[None], sw[None], 0).view(torch.int16), C.view(torch.int16))
 
 
+# Up to a round of workgroups of 16, 32 and 64 columns of 32 rows, and past it.
+@pytest.mark.parametrize("M, Kd, N", [(200, 2688, 672), (300, 2688, 680), (700, 2688, 672), (740, 2688, 672),
+                                      (384, 4096, 664), (250, 4080, 1024), (8192, 256, 24), (4096, 272, 56),
+                                      (4097, 1040, 40), (257, 240, 1000), (100, 1024, 4096), (30, 512, 16384)])
+def test_latent_proj_i8_of_some_rows(M, Kd, N):
+    test_latent_proj_i8(M, Kd, N)
+
+
 def ffn_inputs(counts, D, F, seed):
     g = gen(seed)
     E, R = len(counts), sum(counts)
