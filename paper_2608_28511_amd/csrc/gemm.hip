@@ -1752,6 +1752,10 @@ hipError_t launch_grouped_rows_i8(const int8_t* A, const float* a_scale, const i
                                   hipStream_t st) {
     if (R == 0) return hipSuccess;
     if (Kd <= 0 || Kd % 16 != 0 || N % 8 != 0) return hipErrorInvalidValue;
+    if (sched != nullptr && rows_thin_pays(E, R)) {
+        const SchedPart t = sched_part((void*)sched, E, R, false);
+        return launch_rows_thin(A, a_scale, B, b_scale, C, relu2, t.tiles, t.max_tiles, E, R, N, Kd, st);
+    }
     // two codes to a 16-bit element: the bf16 tiles of half the contraction
     GemmArgs a{};
     a.A = (const uint16_t*)A;

@@ -123,6 +123,11 @@ constexpr int kProjKd = 4096;   // longest row
 bool proj_few_fits(int64_t M, int N, int Kd);
 hipError_t launch_proj_few(const moe_bf16* A, const int8_t* W, const float* w_scale, int64_t M, int N, int Kd,
                            moe_bf16* C, hipStream_t st);
+// launch_grouped_rows_i8 over the 128-row tile table for experts with few rows (thin.hip), where rows_thin_pays.
+bool rows_thin_pays(int E, int64_t R);
+hipError_t launch_rows_thin(const int8_t* A, const float* a_scale, const int8_t* W, const float* w_scale, void* C,
+                            bool relu2, const int4* tiles, int max_tiles, int E, int64_t R, int N, int Kd,
+                            hipStream_t st);
 // 8-bit rows: scale[r] = max|x[r, :]| / 127 and the codes of x[r, :] (quant.hip).  With sched (and offsets
 // [E+1] of the same rows), the launch also builds the grouped GEMM's tile tables.
 hipError_t launch_quant_rows(const moe_bf16* x, int64_t R, int D, int8_t* q, float* scale, hipStream_t st,

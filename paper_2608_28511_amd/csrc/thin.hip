@@ -139,4 +139,54 @@ hipError_t launch_proj_few(const moe_bf16* A, const int8_t* W, const float* w_sc
     return launch_check(st);
 }
 
+// The grouped 8-bit product where experts have few rows: a workgroup takes one entry of the tile table, at most
+// 128 rows of an expert, and one slab of 32 columns.  Its four waves share the contraction of up to 32 rows; of
+// more rows, each takes 32 and the whole contraction, and nothing waits for another wave.
+struct RowsThin {
+    const int8_t* A;
+    const float* a_scale;
+    const int8_t* W;
+    const float* w_scale;
+    uint16_t* C;
+    const int4* tiles;
+    int Kd, N, groups, epi;
+};
+template <bool NT>
+__global__ __launch_bounds__(kThinThreads, 4) void rows_thin_kernel(RowsThin p) {
+    using T = ThinI8<2, NT>;
+    __shared__ __attribute__((aligned(16))) char lds[4 * T::kWaveLds];
+    const int tile = blockIdx.x / p.groups, n0 = blockIdx.x % p.groups * T::kCols;
+    const int4 t = p.tiles[tile];
+    const int e = __builtin_amdgcn_readfirstlane(t.x), row0 = __builtin_amdgcn_readfirstlane(t.y);
+    if (e < 0) return;
+    const int nrows = __builtin_amdgcn_readfirstlane(t.z) - row0;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool few = nrows <= 32;
+    const int r0 = few ? 0 : 32 * wave, n = min(nrows - r0, 32);
+    if (n <= 0) return;
+    const int64_t row = row0 + r0;
+    const ThinArgs a{p.A + row * p.Kd, p.W + (int64_t)e * p.N * p.Kd, p.C + row * p.N, p.a_scale + row,
+                     p.w_scale + (int64_t)e * p.N, (int64_t)n * p.Kd, (int64_t)p.N * p.Kd, p.Kd, p.Kd, p.N, p.epi};
+    thin_rows<T, 2>(a, n0, few ? wave : 0, few ? 4 : 1, n, [](int i) { return i; }, [](int i) { return i; }, lds);
+}
+
+// Up to 12 rows an expert on average.  The expert FFN in us, by the tiles of gemm.hip / this, even loads of 8
+// rows an expert, of 12, Zipf(1.1) loads of 12: 128 experts of 2,048 x 1,024 117 / 102, 119 / 108, 116 / 113; 24
+// of 2,688 x 3,520 129 / 91, 130 / 99, 129 / 104; 40 of 1,040 x 2,000 65 / 49, 66 / 51, 67 / 56; 96 of 512 x
+// 1,024 35 / 31, 36 / 34, 35 / 38; 8 of 512 x 1,024, of 8 rows, 21.3 / 13.4.  Past it: 128 experts of 16 rows
+// 122 / 116 and, Zipf, 120 / 126; 24 rows 128 / 142.  All rows with one of 256 experts (2,048 rows) 33 / 40.
+bool rows_thin_pays(int E, int64_t R) { return R <= 12 * (int64_t)E; }
+
+hipError_t launch_rows_thin(const int8_t* A, const float* a_scale, const int8_t* W, const float* w_scale, void* C,
+                            bool relu2, const int4* tiles, int max_tiles, int E, int64_t R, int N, int Kd,
+                            hipStream_t st) {
+    const int groups = (N + ThinI8<2, false>::kCols - 1) / ThinI8<2, false>::kCols;
+    const RowsThin p{A, a_scale, W, w_scale, (uint16_t*)C, tiles, Kd, N, groups, relu2 ? THIN_RELU2 : THIN_BF16};
+    const dim3 grid((unsigned)(max_tiles * groups)), block(kThinThreads);
+    const bool nt = thin_nt(W, Kd, 2 * (R < E ? R : E) * N * Kd);   // the other projection's weights as many
+    if (nt) hipLaunchKernelGGL(rows_thin_kernel<true>, grid, block, 0, st, p);
+    else hipLaunchKernelGGL(rows_thin_kernel<false>, grid, block, 0, st, p);
+    return launch_check(st);
+}
+
 }  // namespace moe

@@ -175,6 +175,43 @@ def ffn_inputs(counts, D, F, seed):
     return randn(g, R, D), offsets_of(counts), W1q, s1, W2q, s2
 
 
+FEW_ROWS = [[0] * 30 + [129] + [1] * 5 + [33, 0, 64, 0, 0, 2], [16] * 7 + [17] + [0] * 9 + [32, 5, 8],
+            [0] * 90 + [700], [1] * 300, [12] * 5, [96, 31, 0, 0, 0, 97, 1, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0]]
+
+
+@pytest.mark.parametrize("epilogue", [0, 1])
+@pytest.mark.parametrize("Kd, N", [(16, 8), (272, 104), (1040, 40), (2048, 72)])
+@pytest.mark.parametrize("counts", FEW_ROWS)
+def test_experts_of_few_rows(counts, Kd, N, epilogue):
+    """Up to 12 rows an expert on average, some with many: other kernels than for more."""
+    assert sum(counts) <= 12 * len(counts)
+    test_grouped_gemm_i8(counts, Kd, N, epilogue)
+
+
+@pytest.mark.parametrize("D, F", [(2048, 1024), (1040, 2064)])
+def test_experts_of_few_rows_past_the_last_level_cache(D, F):
+    """Their weights over 256 MB are read another way, where their rows start on cache lines.  The same rows
+    among as many more as take them to the tiles of larger calls give the same."""
+    E = 80
+    counts = [(7 * e) % 23 for e in range(E)]
+    x, offsets, W1q, s1, W2q, s2 = ffn_inputs(counts, D, F, 31)
+    y = layer.grouped_ffn_i8(x, offsets, W1q, s1, W2q, s2)
+    more = torch.cat([x, randn(gen(32), 1000, D)])
+    off = torch.cat([offsets[:-1], offsets[-1:] + 1000])
+    z = layer.grouped_ffn_i8(more, off, W1q, s1, W2q, s2)
+    assert sum(counts) <= 12 * E < len(more)
+    assert torch.equal(y, z[:len(x)])
+
+
+def test_few_rows_leave_the_rows_behind_them():
+    counts = [3, 0, 33, 1]
+    x, offsets, W1q, s1, W2q, s2 = ffn_inputs(counts, 48, 80, 33)
+    R, q = 45, layer.quant_rows_i8(torch.cat([x, x[:8]]))
+    C = torch.full((R, 80), -7.0, dtype=BF16, device=DEV)
+    layer.grouped_gemm_i8(*q, layer.grouped_schedule(offsets, 4, R), W1q, s1, 1, out=C)
+    assert bool((C[37:] == -7).all()) and not bool((C[:37] == -7).any())
+
+
 FFNS = [([1], 16, 16), ([0, 1, 0, 0], 48, 80), ([3, 0, 200, 129, 1], 272, 336), ([700, 2, 0, 1500], 512, 1040),
         ([0, 4000, 3500, 0], 2064, 1024)]
 
