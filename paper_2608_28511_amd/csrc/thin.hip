@@ -140,7 +140,7 @@ hipError_t launch_proj_few(const moe_bf16* A, const int8_t* W, const float* w_sc
 }
 
 // The grouped 8-bit product where experts have few rows: a workgroup takes one entry of the tile table, at most
-// 128 rows of an expert, and one slab of 32 columns.  Its four waves share the contraction of up to 32 rows; of
+// 128 rows of an expert, and one slab of 16 NB columns.  Its four waves share the contraction of up to 32 rows; of
 // more rows, each takes 32 and the whole contraction, and nothing waits for another wave.
 struct RowsThin {
     const int8_t* A;
@@ -151,9 +151,9 @@ struct RowsThin {
     const int4* tiles;
     int Kd, N, groups, epi;
 };
-template <bool NT>
-__global__ __launch_bounds__(kThinThreads, 4) void rows_thin_kernel(RowsThin p) {
-    using T = ThinI8<2, NT>;
+template <int NB, bool NT>
+__global__ __launch_bounds__(kThinThreads, NB == 2 ? 4 : 3) void rows_thin_kernel(RowsThin p) {
+    using T = ThinI8<NB, NT>;
     __shared__ __attribute__((aligned(16))) char lds[4 * T::kWaveLds];
     const int tile = blockIdx.x / p.groups, n0 = blockIdx.x % p.groups * T::kCols;
     const int4 t = p.tiles[tile];
@@ -170,22 +170,30 @@ __global__ __launch_bounds__(kThinThreads, 4) void rows_thin_kernel(RowsThin p) 
     thin_rows<T, 2>(a, n0, few ? wave : 0, few ? 4 : 1, n, [](int i) { return i; }, [](int i) { return i; }, lds);
 }
 
-// Up to 12 rows an expert on average.  The expert FFN in us, by the tiles of gemm.hip / this, even loads of 8
-// rows an expert, of 12, Zipf(1.1) loads of 12: 128 experts of 2,048 x 1,024 117 / 102, 119 / 108, 116 / 113; 24
-// of 2,688 x 3,520 129 / 91, 130 / 99, 129 / 104; 40 of 1,040 x 2,000 65 / 49, 66 / 51, 67 / 56; 96 of 512 x
-// 1,024 35 / 31, 36 / 34, 35 / 38; 8 of 512 x 1,024, of 8 rows, 21.3 / 13.4.  Past it: 128 experts of 16 rows
-// 122 / 116 and, Zipf, 120 / 126; 24 rows 128 / 142.  All rows with one of 256 experts (2,048 rows) 33 / 40.
-bool rows_thin_pays(int E, int64_t R) { return R <= 12 * (int64_t)E; }
+// Up to 20 rows an expert on average.  90 random expert FFNs (8 to 256 experts, 256 to 2,688 by 512 to 3,712, even
+// and Zipf loads) take of the tiles' time, by rows an expert: 4 to 8 0.65, 8 to 12 0.77, 12 to 16 0.81, 16 to
+// 20 0.85 (of single ones at most 0.99), 20 to 24 0.89 (1.04).  In us, tiles / this, even loads of 8 rows: 128 experts
+// of 2,048 x 1,024 117 / 103; 24 of 2,688 x 3,520 129 / 91; 8 of 512 x 1,024 21.3 / 13.4; and the other way, 3,001 rows
+// among those 128 by Zipf(1.1) 141 / 157, all 2,048 rows with one of 256 experts of 1,024 x 1,024 33 / 40.
+bool rows_thin_pays(int E, int64_t R) { return R <= 20 * (int64_t)E; }
+
+// Columns of a slab.  64 read the rows half as often as 32, which pays where there are more than 12 an expert, unless
+// so few weights that the workgroups are few (64 MB: of the tiles' time with 32 / 64 columns, 12 to 20 rows, more
+// weights 0.87 / 0.85, fewer 0.81 / 0.89; 8 to 12 rows 0.77 / 0.82).
+static int rows_thin_cols(int E, int64_t R, int N, int Kd) {
+    return R > 12 * (int64_t)E && (int64_t)E * N * Kd > (int64_t)64 << 20 ? 64 : 32;
+}
 
 hipError_t launch_rows_thin(const int8_t* A, const float* a_scale, const int8_t* W, const float* w_scale, void* C,
                             bool relu2, const int4* tiles, int max_tiles, int E, int64_t R, int N, int Kd,
                             hipStream_t st) {
-    const int groups = (N + ThinI8<2, false>::kCols - 1) / ThinI8<2, false>::kCols;
+    const int cols = rows_thin_cols(E, R, N, Kd), groups = (N + cols - 1) / cols;
     const RowsThin p{A, a_scale, W, w_scale, (uint16_t*)C, tiles, Kd, N, groups, relu2 ? THIN_RELU2 : THIN_BF16};
     const dim3 grid((unsigned)(max_tiles * groups)), block(kThinThreads);
     const bool nt = thin_nt(W, Kd, 2 * (R < E ? R : E) * N * Kd);   // the other projection's weights as many
-    if (nt) hipLaunchKernelGGL(rows_thin_kernel<true>, grid, block, 0, st, p);
-    else hipLaunchKernelGGL(rows_thin_kernel<false>, grid, block, 0, st, p);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, p); };
+    if (cols == 32) nt ? go(rows_thin_kernel<2, true>) : go(rows_thin_kernel<2, false>);
+    else nt ? go(rows_thin_kernel<4, true>) : go(rows_thin_kernel<4, false>);
     return launch_check(st);
 }
 

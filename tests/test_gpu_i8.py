@@ -183,7 +183,7 @@ FEW_ROWS = [[0] * 30 + [129] + [1] * 5 + [33, 0, 64, 0, 0, 2], [16] * 7 + [17] +
 @pytest.mark.parametrize("Kd, N", [(16, 8), (272, 104), (1040, 40), (2048, 72)])
 @pytest.mark.parametrize("counts", FEW_ROWS)
 def test_experts_of_few_rows(counts, Kd, N, epilogue):
-    """Up to 12 rows an expert on average, some with many: other kernels than for more."""
+    """Few rows an expert on average, some with many: other kernels than for more."""
     assert sum(counts) <= 12 * len(counts)
     test_grouped_gemm_i8(counts, Kd, N, epilogue)
 
@@ -196,11 +196,24 @@ def test_experts_of_few_rows_past_the_last_level_cache(D, F):
     counts = [(7 * e) % 23 for e in range(E)]
     x, offsets, W1q, s1, W2q, s2 = ffn_inputs(counts, D, F, 31)
     y = layer.grouped_ffn_i8(x, offsets, W1q, s1, W2q, s2)
-    more = torch.cat([x, randn(gen(32), 1000, D)])
-    off = torch.cat([offsets[:-1], offsets[-1:] + 1000])
+    more = torch.cat([x, randn(gen(32), 2000, D)])
+    off = torch.cat([offsets[:-1], offsets[-1:] + 2000])
     z = layer.grouped_ffn_i8(more, off, W1q, s1, W2q, s2)
-    assert sum(counts) <= 12 * E < len(more)
+    assert sum(counts) <= 12 * E and 20 * E < len(more)
     assert torch.equal(y, z[:len(x)])
+
+
+@pytest.mark.parametrize("D, F", [(1040, 1096), (2048, 1024)])
+def test_experts_of_some_rows_and_large_weights(D, F):
+    """13 to 20 rows an expert on average, weights of 64 to 128 and past 128 MB; against the tiles of larger calls."""
+    for E, per in ((64, 14), (80, 19)):
+        counts = [(11 * e) % (2 * per) for e in range(E)]
+        x, offsets, W1q, s1, W2q, s2 = ffn_inputs(counts, D, F // 16 * 16, 41)
+        assert 12 * E < sum(counts) <= 20 * E and E * D * F > 2 ** 26
+        more = torch.cat([x, randn(gen(42), 20 * E, D)])
+        off = torch.cat([offsets[:-1], offsets[-1:] + 20 * E])
+        y = layer.grouped_ffn_i8(x, offsets, W1q, s1, W2q, s2)
+        assert torch.equal(y, layer.grouped_ffn_i8(more, off, W1q, s1, W2q, s2)[:len(x)])
 
 
 def test_few_rows_leave_the_rows_behind_them():
