@@ -676,8 +676,9 @@ size_t moe_layer_few_workspace_bytes(const moe_layer_few_args* a);
  * layer (no latent projection) for S <= 64 tokens, without a permutation.  Picks and
  * weights follow moe_route_topk or moe_route_sigmoid on fp32-accurate logits; sums over
  * the K experts and the shared expert are fp32 with one rounding, to y.  Expert
- * activations are rounded to bf16 (and, with 8-bit weights, quantised as in
- * moe_grouped_ffn_i8).  The logits' last bits may differ from moe_router_logits'.
+ * activations are held to 2^-16 of their value; with 8-bit weights they are rounded
+ * to bf16 and quantised as in moe_grouped_ffn_i8.  The logits' last bits may differ
+ * from moe_router_logits'.
  * With 8-bit weights D, F and Fs are multiples of 16.
  * Errors: MOE_ERR_SHAPE for sizes (S > MOE_FEW_MAX_TOKENS among them), unknown modes,
  * sel_bias with softmax scores, and shared weights or scales where there are none to

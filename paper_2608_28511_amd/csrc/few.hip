@@ -9,7 +9,11 @@
 //   few_route    one workgroup a token: the partial sums, top-K and weights; with 8-bit
 //                weights as many again quantise the token rows
 //   few_table    many picks: the picked experts' rows, else found by each workgroup below
-//   few_gemm     up: h = bf16(max(x W1, 0)^2)
+//   few_gemm     up: h = max(x W1, 0)^2, rounded to bf16 with 8-bit weights (then to codes); with bf16
+//                weights in two bf16 parts, within 2^-16, so that the only rounding to bf16 is y's: a
+//                second matrix instruction a fragment in the down product, 0 to 4% of a call that
+//                reads its weights (64 tokens of 64 experts 107 / 111 us, 8 of the production layer
+//                286 / 290; 64 tokens on two experts of 2,048 x 4,096 58 / 73)
 //   few_quant    8-bit weights: the rows of h
 //   few_gemm     down: y_k = h W2 in fp32
 //   few_combine  y = bf16(sum_k p_k y_k + shared), all sums in fp32 and fixed order
@@ -558,8 +562,8 @@ FewPlan few_plan_of(const moe_layer_few_args* a) {
     p.rows = take(p.table ? R * 4 : 0);
     p.xq = take(i8 ? (size_t)S * D : 0);
     p.xs = take((size_t)S * 4);
-    p.h = take(R * F * 2);
-    p.hs = take((size_t)S * Fs * 2);
+    p.h = take(R * F * (i8 ? 2 : 4));   // bf16 weights: two parts
+    p.hs = take((size_t)S * Fs * (i8 ? 2 : 4));
     p.hq = take(i8 ? R * F : 0);
     p.hqs = take(i8 ? (size_t)S * Fs : 0);
     p.sc = take(R * 4);
@@ -613,9 +617,11 @@ hipError_t launch_layer_few(const moe_layer_few_args* a, hipStream_t st) {
     if (p.table)
         hipLaunchKernelGGL(few_table_kernel, dim3(1), dim3(kTableThreads), 0, st, idx, R, p.r_experts,
                            (int4*)(ws + p.tab), (int32_t*)(ws + p.rows));
-    auto gemm = [&](FewSide r, FewSide s, int wk, int epi) {
+    // parts: of the values of A, where weights are bf16
+    auto gemm = [&](auto parts, FewSide r, FewSide s, int wk, int epi) {
+        constexpr int PARTS = decltype(parts)::value;
         for (FewSide* q : {&r, &s}) {
-            q->lda = q->Kd * wb;
+            q->lda = q->Kd * (i8 ? 1 : 2 * PARTS);
             q->a_bytes *= q->lda;                       // given as rows
             q->w_bytes = (int64_t)q->Kd * q->N * wb;
             q->groups = cdiv(cdiv(q->N, cols), 4 / wk);
@@ -626,8 +632,8 @@ hipError_t launch_layer_few(const moe_layer_few_args* a, hipStream_t st) {
         auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, g); };
         auto pick = [&](auto nt) {
             constexpr bool NT = decltype(nt)::value;
-            if (S <= 16) i8 ? go(few_gemm_kernel<ThinI8<2, NT>, 1>) : go(few_gemm_kernel<ThinBf16<NT>, 1>);
-            else if (!i8) go(few_gemm_kernel<ThinBf16<NT>, 4>);
+            if (S <= 16) i8 ? go(few_gemm_kernel<ThinI8<2, NT>, 1>) : go(few_gemm_kernel<ThinBf16<NT, PARTS>, 1>);
+            else if (!i8) go(few_gemm_kernel<ThinBf16<NT, PARTS>, 4>);
             else if (S <= 32)
                 cols == kSlabI8 ? go(few_gemm_kernel<ThinI8<2, NT>, 2>) : go(few_gemm_kernel<ThinI8<4, NT>, 2>);
             else cols == kSlabI8 ? go(few_gemm_kernel<ThinI8<2, NT>, 4>) : go(few_gemm_kernel<ThinI8<4, NT>, 4>);
@@ -637,8 +643,8 @@ hipError_t launch_layer_few(const moe_layer_few_args* a, hipStream_t st) {
     };
     // A, W, out, row and column scales, rows of A, .., .., a_div, Kd, N (the rest is set above)
     const void* x = i8 ? (const void*)xq : (const void*)a->x;
-    gemm(FewSide{x, a->W1, h, xs, a->s1, S, 0, 0, K, D, F, 0}, FewSide{x, a->Ws1, hs, xs, a->ss1, S, 0, 0, 1, D, Fs, 0},
-         p.wk1, THIN_RELU2);
+    gemm(std::integral_constant<int, 1>{}, FewSide{x, a->W1, h, xs, a->s1, S, 0, 0, K, D, F, 0},
+         FewSide{x, a->Ws1, hs, xs, a->ss1, S, 0, 0, 1, D, Fs, 0}, p.wk1, THIN_RELU2);
     const void *hr = h, *hsr = hs;
     if (i8) {
         const FewRows qr{h, hq, sc, F, R}, qs{hs, hqs, scs, Fs, Fs ? S : 0};
@@ -646,9 +652,8 @@ hipError_t launch_layer_few(const moe_layer_few_args* a, hipStream_t st) {
         hr = hq;
         hsr = hqs;
     }
-    gemm(FewSide{hr, a->W2, y, sc, a->s2, R, 0, 0, 1, F, D, 0},
-         FewSide{hsr, a->Ws2, ys, scs, a->ss2, S, 0, 0, 1, Fs, D, 0},
-         p.wk2, THIN_F32);
+    gemm(std::integral_constant<int, 2>{}, FewSide{hr, a->W2, y, sc, a->s2, R, 0, 0, 1, F, D, 0},
+         FewSide{hsr, a->Ws2, ys, scs, a->ss2, S, 0, 0, 1, Fs, D, 0}, p.wk2, THIN_F32);
     hipLaunchKernelGGL(few_combine_kernel, dim3((unsigned)cdiv(D, 256), (unsigned)S), dim3(kFewThreads), 0, st, y,
                        Fs ? ys : nullptr, prob, K, D, a->y);
     return launch_check(st);

@@ -23,14 +23,15 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t thin_rsrc(const void* base, in
     return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int32_t)bytes, 0x00020000);
 }
 
-// What leaves a product: fp32, or bf16 of it, or bf16 of its squared ReLU.
+// What leaves a product: fp32, or bf16 of it, or its squared ReLU, in bf16 with 8-bit weights and
+// in two bf16 parts with bf16 ones.
 enum { THIN_F32 = 0, THIN_BF16 = 1, THIN_RELU2 = 2 };
 
 // One expert's product.
 struct ThinArgs {
     const void* A;              // its rows start within a_bytes
     const void* W;              // bf16 [Kd, N] or int8 [N, Kd]
-    void* out;                  // [rows][N]
+    void* out;                  // [rows][N]; in two parts [rows][N / 8][2][8]
     const float* row_scale;     // 8-bit: by source row
     const float* col_scale;     // 8-bit: [N]
     int64_t a_bytes, w_bytes;
@@ -42,14 +43,15 @@ struct ThinArgs {
 // bf16 weights, N-contiguous: slabs of 64 columns, steps of 32 k.  A lane loads 4
 // columns of 8 k rows (each load of the wave four whole cache lines) and packs them into
 // the fragments of columns 4 c + q, q = 0 .. 3, with one byte permutation a register.  NT:
-// non-temporal loads (see thin_nt).
-template <bool NT>
+// non-temporal loads (see thin_nt).  PARTS: bf16 parts of A's values, whose products are
+// summed; a row of A holds the first parts of eight values, then their second ones.
+template <bool NT, int PARTS = 1>
 struct ThinBf16 {
     static constexpr bool kI8 = false;
     static constexpr int kCols = 64, kStep = 32, kAcc = 4;
     static constexpr int kWaveLds = kAcc * 1024;   // bytes: the wave's sums
     template <int MB>
-    static constexpr int kAhead = MB == 4 ? 3 : 4;
+    static constexpr int kAhead = MB == 4 || PARTS == 2 ? 3 : 4;
     u32x2_thin w[8];
 
     __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t& rw, const ThinArgs& s, int n0, int k, int lane) {
@@ -61,13 +63,16 @@ struct ThinBf16 {
     }
     template <int MB>
     struct A {
-        u32x4 v[MB];
+        u32x4 v[MB][PARTS];
         __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t& ra, const uint32_t (&row)[MB], int k, int Kd,
                                              int lane) {
             const int kk = k + 8 * (lane >> 4);
 #pragma unroll
             for (int m = 0; m < MB; ++m)
-                v[m] = __builtin_amdgcn_raw_buffer_load_b128(ra, kk < Kd ? row[m] + (uint32_t)kk * 2 : kThinDrop, 0, 0);
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p)
+                    v[m][p] = __builtin_amdgcn_raw_buffer_load_b128(
+                        ra, kk < Kd ? row[m] + (uint32_t)(kk * PARTS + 8 * p) * 2 : kThinDrop, 0, 0);
         }
     };
     template <int MB>
@@ -80,7 +85,10 @@ struct ThinBf16 {
                 f[u] = __builtin_amdgcn_perm(w[2 * u + 1][q >> 1], w[2 * u][q >> 1], q & 1 ? 0x07060302u : 0x05040100u);
 #pragma unroll
             for (int m = 0; m < MB; ++m)
-                acc[m][q] = mfma16<false>(__builtin_bit_cast(bf16x8, f), __builtin_bit_cast(bf16x8, a.v[m]), acc[m][q]);
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p)
+                    acc[m][q] =
+                        mfma16<false>(__builtin_bit_cast(bf16x8, f), __builtin_bit_cast(bf16x8, a.v[m][p]), acc[m][q]);
         }
     }
     // acc[q][v] of a lane is column 16 g + 4 v + q of its token: piece v is four columns
@@ -253,7 +261,20 @@ __device__ __forceinline__ void thin_body(const ThinArgs& s, int n0, int kk, int
                     t[q] *= t[q];
                 }
             }
-            *(u32x2_thin*)((uint16_t*)s.out + at) = u32x2_thin{pack_bf16x2(t[0], t[1]), pack_bf16x2(t[2], t[3])};
+            uint16_t* o = (uint16_t*)s.out + at;
+            if constexpr (!T::kI8) {
+                // the value's first eight bits, and the rest rounded to as many: within 2^-16 of it
+                o += at - (col & 4);
+                f32x4 rest;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float first = __uint_as_float(__float_as_uint(t[q]) & 0xffff0000u);
+                    rest[q] = fmaxf(t[q] - first, 0.f);   // an infinity or a NaN leaves none
+                    t[q] = first;
+                }
+                *(u32x2_thin*)(o + 8) = u32x2_thin{pack_bf16x2(rest[0], rest[1]), pack_bf16x2(rest[2], rest[3])};
+            }
+            *(u32x2_thin*)o = u32x2_thin{pack_bf16x2(t[0], t[1]), pack_bf16x2(t[2], t[3])};
         }
     };
 #pragma unroll

@@ -356,3 +356,38 @@ def test_refusals_on_the_device():
         m.layer(65)
     with pytest.raises(ValueError):
         layer.LayerFew(4, m.Wr, m.W1, m.W2, 2, sel_bias=m.bias, score="softmax")
+
+
+def parts_bound(x, W1, W2):
+    """(y, b) of one bf16 expert as serving_oracle.ffn_bound gives them, with h within 2^-16 and an fp32 rounding
+    of itself and sums of its two parts."""
+    x, W1, W2 = (np.asarray(a, np.float64) for a in (x, W1, W2))
+    D, F = W1.shape
+    u = np.maximum(x @ W1, 0.0)
+    du = D * 2.0 ** -24 * (np.abs(x) @ np.abs(W1))
+    h = u * u
+    dh = 2 * u * du + du * du + (2.0 ** -16 + 2.0 ** -23) * (u + du) ** 2
+    return h @ W2, dh @ np.abs(W2) + 2 * F * 2.0 ** -24 * ((h + dh) @ np.abs(W2))
+
+
+@pytest.mark.parametrize("S, D, E, K, F, Fs, score", SHAPES)
+def test_hidden_values_keep_more_than_bf16(S, D, E, K, F, Fs, score, monkeypatch):
+    """With bf16 weights, y is one rounding to bf16 away from the fp32 layer's."""
+    monkeypatch.setattr(V, "ffn_bound", parts_bound)
+    m = Model(D, E, K, F, Fs, score, seed=S + E + 1)
+    x = m.tokens(S)
+    check_bf16(m, x, m.layer(S)(x))
+
+
+def test_hidden_values_at_the_end_of_the_range():
+    """Hidden values past the largest bf16 are finite where fp32 holds them; past fp32 they are infinite."""
+    D = F = 16
+    W1, W2 = torch.zeros((1, D, F), device=DEV), torch.zeros((1, F, D), device=DEV)
+    W1[0, 0, 0] = W1[0, 1, 0] = W1[0, 3, 1] = 1.0
+    W2[0, 0, 0], W2[0, 1, 1] = 2.0 ** -100, 1.0
+    x = torch.zeros((2, D), device=DEV)
+    x[0, 0], x[0, 1] = 2.0 ** 64, -2.0 ** 52      # h = 2^128 (1 - 2^-11 + 2^-24): fp32 holds it, bf16 rounds it up
+    x[1, 3] = 2.0 ** 64                           # h = 2^128
+    y = layer.LayerFew(2, torch.zeros((D, 1), device=DEV), W1.to(BF16), W2.to(BF16), 1)(x.to(BF16))["y"]
+    assert float(y[0, 0]) == 2.0 ** 28 and not bool(y[0, 1:].any())
+    assert float(y[1, 1]) == float("inf")
