@@ -46,10 +46,10 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_cvt){lo, hi}, bf16x2_cvt));
 }
 
-// max(x, 0) as one integer max of the bit pattern: every negative value and
-// -0 map to +0, non-negative values pass unchanged (a NaN with the sign bit
-// clear passes too).  fmaxf costs a NaN-quieting max on top.
-__device__ __forceinline__ float relu_f32(float x) { return __int_as_float(max(__float_as_int(x), 0)); }
+// max(x, 0) in one instruction that hands every NaN on, whatever its sign, and
+// gives +0 for -0.  (fmaxf drops a NaN, and an integer max of the bit patterns
+// those with the sign bit set, as the matrix cores' are.)
+__device__ __forceinline__ float relu_f32(float x) { return __builtin_elementwise_maximum(x, 0.f); }
 
 // MOE_DEBUG_SYNC=1 in the environment (read once per process).
 bool debug_sync_enabled();

@@ -1,0 +1,111 @@
+"""A NaN passes the squared ReLU and its derivative, whatever its sign bit (the matrix
+cores' NaNs have it set, and so has what 0 / 0 gives on an x86 host); every other value
+keeps its bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_28511_amd import layer
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16 = torch.bfloat16
+SIZES = [(37, 64, 48), (300, 264, 200), (9000, 1040, 1032)]   # R, D, F: from one narrow tile to the 256-row ones
+
+
+def bad(*signs):
+    """bf16 NaNs, by sign."""
+    return torch.tensor([(0xffc0 if s < 0 else 0x7fc0) - (0x10000 if s < 0 else 0) for s in signs],
+                        dtype=torch.int16, device=DEV).view(BF16)
+
+
+def inputs(R, D, F, E=2, seed=0):
+    g = torch.Generator(device=DEV).manual_seed(R + seed)
+    n = lambda *s, std=1.0: (torch.randn(s, generator=g, device=DEV) * std).to(BF16)  # noqa: E731
+    off = torch.tensor([0, R // 3, R], dtype=torch.int32, device=DEV)
+    return n(R, D), off, n(E, D, F, std=D ** -0.5), n(E, F, D, std=F ** -0.5), n(R, D)
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("R, D, F", SIZES)
+def test_expert_ffn(R, D, F, sign):
+    x, off, W1, W2, _ = inputs(R, D, F)
+    h0, _, y0 = layer.grouped_ffn(x, off, W1, W2, save_u=True)
+    x[R - 2, 5] = bad(sign)[0]
+    h, _, y = layer.grouped_ffn(x, off, W1, W2, save_u=True)
+    keep = torch.arange(R, device=DEV) != R - 2
+    assert bool(torch.isnan(h[R - 2]).all()) and bool(torch.isnan(y[R - 2]).all())
+    assert torch.equal(h[keep], h0[keep]) and torch.equal(y[keep], y0[keep])
+    # a weight: its output column, for the rows of its expert
+    x, off, W1, W2, _ = inputs(R, D, F)
+    W1[1, 3, F - 1] = bad(sign)[0]
+    h = layer.grouped_ffn(x, off, W1, W2, save_u=False)[0]
+    hit = torch.zeros((R, F), dtype=torch.bool, device=DEV)
+    hit[R // 3:, F - 1] = True
+    assert torch.equal(torch.isnan(h), hit) and torch.equal(h[~hit], h0[~hit])
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("R, D, F", SIZES)
+def test_expert_ffn_backward(R, D, F, sign):
+    x, off, W1, W2, dy = inputs(R, D, F)
+    h, u, _ = layer.grouped_ffn(x, off, W1, W2, save_u=True)
+    dx0 = layer.grouped_ffn_bwd(x, u, h, dy, off, W1, W2)[0]
+    u[1, 7] = bad(sign)[0]
+    dx, dW1, _ = layer.grouped_ffn_bwd(x, u, h, dy, off, W1, W2)
+    assert bool(torch.isnan(dx[1]).all()) and bool(torch.isnan(dW1[0, :, 7]).all())
+    assert torch.equal(dx[2:], dx0[2:]) and not bool(torch.isnan(dW1[1]).any())
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+def test_shared_expert(sign):
+    x, _, W1, W2, _ = inputs(100, 64, 48)
+    x[9, 0] = bad(sign)[0]
+    h, _, y = layer.shared_expert_fwd(x, W1[0], W2[0])
+    nan = torch.isnan(h).all(1)
+    assert bool(nan[9]) and int(nan.sum()) == 1 and bool(torch.isnan(y[9]).all())
+    assert int(torch.isnan(y).sum()) == 64
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("S", [1, 9, 40])
+def test_few_tokens(S, sign):
+    x, _, W1, W2, _ = inputs(S, 64, 48)
+    Wr = torch.zeros((64, 2), device=DEV)
+    W1[1, 3, 5] = bad(sign)[0]
+    bias = torch.tensor([0.0, -1.0], device=DEV)
+    assert bool(torch.isnan(layer.LayerFew(S, Wr, W1, W2, 2, bias=bias)(x)["y"]).all())   # both experts
+    assert not bool(torch.isnan(layer.LayerFew(S, Wr, W1, W2, 1, bias=bias)(x)["y"]).any())   # the other one alone
+
+
+@pytest.mark.parametrize("rows", [30, 3000])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_8_bit_products(rows, sign):
+    """A scale that is such a NaN."""
+    g = torch.Generator(device=DEV).manual_seed(rows)
+    q, W = (torch.randint(1, 128, s, generator=g, device=DEV, dtype=torch.int32).to(torch.int8)
+            for s in ((rows, 64), (1, 48, 64)))
+    sa, sw = torch.ones(rows, device=DEV), torch.ones((1, 48), device=DEV)
+    sa[3] = bad(sign).float()[0]
+    off = torch.tensor([0, rows], dtype=torch.int32, device=DEV)
+    for sched in (layer.grouped_schedule(off, 1, rows), None):
+        C = layer.grouped_gemm_i8(q, sa, sched, W, sw, 1)
+        assert bool(torch.isnan(C[3]).all()) and int(torch.isnan(C).sum()) == 48
+
+
+def test_other_values_keep_their_bits():
+    """Every bf16 value once through the squared ReLU of a product with the identity."""
+    v = np.arange(1 << 16, dtype=np.uint16)
+    x = torch.tensor(v.view(np.int16), device=DEV).view(BF16)
+    fine = torch.isfinite(x)
+    D = 64
+    rows = torch.zeros((1 << 16, D), dtype=BF16, device=DEV)
+    rows[:, 0] = torch.where(fine, x, torch.zeros_like(x))   # a NaN or an infinity would meet zero weights
+    W = torch.eye(D, device=DEV).to(BF16)[None].contiguous()
+    off = torch.tensor([0, 1 << 16], dtype=torch.int32, device=DEV)
+    h = layer.grouped_gemm(rows, layer.grouped_schedule(off, 1, 1 << 16), W, 1)
+    ref = (rows[:, 0].double().clamp_min(0) ** 2)
+    normal = ref >= 2.0 ** -126          # squares below are subnormal, or zero
+    assert torch.equal(h[normal, 0], ref[normal].float().to(BF16))
+    assert bool((h[~normal, 0].double() <= 2.0 ** -126).all()) and not bool(h[:, 1:].any())
+    assert not bool((h.view(torch.int16) < 0).any())         # +0, never -0
