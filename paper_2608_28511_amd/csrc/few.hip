@@ -575,7 +575,7 @@ FewPlan few_plan_of(const moe_layer_few_args* a) {
 }
 
 template <int EPL>
-void launch_route_few(bool sig, dim3 g, hipStream_t st, const float* part, int nd, const moe_layer_few_args* a,
+hipError_t launch_route_few(bool sig, dim3 g, hipStream_t st, const float* part, int nd, const moe_layer_few_args* a,
                       int32_t* idx, float* prob, int8_t* xq, float* xs) {
     if (sig)
         hipLaunchKernelGGL((few_route_kernel<EPL, true>), g, dim3(kRouteThreads), 0, st, part, nd, a->router_bias,
@@ -583,7 +583,14 @@ void launch_route_few(bool sig, dim3 g, hipStream_t st, const float* part, int n
     else
         hipLaunchKernelGGL((few_route_kernel<EPL, false>), g, dim3(kRouteThreads), 0, st, part, nd, a->router_bias,
                            a->sel_bias, (int)a->S, a->E, a->K, idx, prob, a->x, a->D, xq, xs);
+    return launch_check(st);
 }
+
+#define FEW_TRY(expr)                    \
+    do {                                 \
+        const hipError_t e_ = (expr);    \
+        if (e_ != hipSuccess) return e_; \
+    } while (0)
 
 }  // namespace
 
@@ -605,18 +612,24 @@ hipError_t launch_layer_few(const moe_layer_few_args* a, hipStream_t st) {
 
     hipLaunchKernelGGL(few_logits_kernel, dim3((unsigned)p.nd, (unsigned)cdiv(E, 64), (unsigned)cdiv(S, kFewT)),
                        dim3(kFewThreads), 0, st, a->x, a->Wr, S, D, E, part);
+    FEW_TRY(launch_check(st));
     const dim3 gr((unsigned)(i8 ? 2 * S : S));
     const bool sig = a->score_fn == MOE_SCORE_SIGMOID;
-    if (E <= 64) launch_route_few<1>(sig, gr, st, part, p.nd, a, idx, prob, xq, xs);
-    else if (E <= 128) launch_route_few<2>(sig, gr, st, part, p.nd, a, idx, prob, xq, xs);
-    else if (E <= 256) launch_route_few<4>(sig, gr, st, part, p.nd, a, idx, prob, xq, xs);
-    else if (E <= 512) launch_route_few<8>(sig, gr, st, part, p.nd, a, idx, prob, xq, xs);
-    else launch_route_few<16>(sig, gr, st, part, p.nd, a, idx, prob, xq, xs);
+    auto route = [&](auto epl) {
+        return launch_route_few<decltype(epl)::value>(sig, gr, st, part, p.nd, a, idx, prob, xq, xs);
+    };
+    FEW_TRY(E <= 64    ? route(std::integral_constant<int, 1>{})
+            : E <= 128 ? route(std::integral_constant<int, 2>{})
+            : E <= 256 ? route(std::integral_constant<int, 4>{})
+            : E <= 512 ? route(std::integral_constant<int, 8>{})
+                       : route(std::integral_constant<int, 16>{}));
 
     const int4* table = p.table ? (const int4*)(ws + p.tab) : nullptr;
-    if (p.table)
+    if (p.table) {
         hipLaunchKernelGGL(few_table_kernel, dim3(1), dim3(kTableThreads), 0, st, idx, R, p.r_experts,
                            (int4*)(ws + p.tab), (int32_t*)(ws + p.rows));
+        FEW_TRY(launch_check(st));
+    }
     // parts: of the values of A, where weights are bf16
     auto gemm = [&](auto parts, FewSide r, FewSide s, int wk, int epi) {
         constexpr int PARTS = decltype(parts)::value;
@@ -640,20 +653,22 @@ hipError_t launch_layer_few(const moe_layer_few_args* a, hipStream_t st) {
         };
         if (thin_nt(r.W, (int64_t)(i8 ? r.Kd : r.N) * wb, 2 * (int64_t)p.r_experts * r.w_bytes)) pick(std::true_type{});
         else pick(std::false_type{});
+        return launch_check(st);
     };
     // A, W, out, row and column scales, rows of A, .., .., a_div, Kd, N (the rest is set above)
     const void* x = i8 ? (const void*)xq : (const void*)a->x;
-    gemm(std::integral_constant<int, 1>{}, FewSide{x, a->W1, h, xs, a->s1, S, 0, 0, K, D, F, 0},
-         FewSide{x, a->Ws1, hs, xs, a->ss1, S, 0, 0, 1, D, Fs, 0}, p.wk1, THIN_RELU2);
+    FEW_TRY(gemm(std::integral_constant<int, 1>{}, FewSide{x, a->W1, h, xs, a->s1, S, 0, 0, K, D, F, 0},
+                 FewSide{x, a->Ws1, hs, xs, a->ss1, S, 0, 0, 1, D, Fs, 0}, p.wk1, THIN_RELU2));
     const void *hr = h, *hsr = hs;
     if (i8) {
         const FewRows qr{h, hq, sc, F, R}, qs{hs, hqs, scs, Fs, Fs ? S : 0};
         hipLaunchKernelGGL(few_quant_kernel, dim3((unsigned)(qr.rows + qs.rows)), dim3(kFewThreads), 0, st, qr, qs);
+        FEW_TRY(launch_check(st));
         hr = hq;
         hsr = hqs;
     }
-    gemm(std::integral_constant<int, 2>{}, FewSide{hr, a->W2, y, sc, a->s2, R, 0, 0, 1, F, D, 0},
-         FewSide{hsr, a->Ws2, ys, scs, a->ss2, S, 0, 0, 1, Fs, D, 0}, p.wk2, THIN_F32);
+    FEW_TRY(gemm(std::integral_constant<int, 2>{}, FewSide{hr, a->W2, y, sc, a->s2, R, 0, 0, 1, F, D, 0},
+                 FewSide{hsr, a->Ws2, ys, scs, a->ss2, S, 0, 0, 1, Fs, D, 0}, p.wk2, THIN_F32));
     hipLaunchKernelGGL(few_combine_kernel, dim3((unsigned)cdiv(D, 256), (unsigned)S), dim3(kFewThreads), 0, st, y,
                        Fs ? ys : nullptr, prob, K, D, a->y);
     return launch_check(st);
