@@ -100,7 +100,8 @@ constexpr int kQw = 64;
 __global__ __launch_bounds__(256) void quant_weights_kernel(const uint16_t* __restrict__ W, int Kd, int N,
                                                             int8_t* __restrict__ Wq, float* __restrict__ scale) {
     __shared__ uint32_t top_s[32][kQw];
-    __shared__ int8_t tile[kQw][kQw + 16];   // [channel][k], rows 16 bytes apart in the banks
+    // [channel][k], rows 16 bytes apart in the banks
+    __shared__ __attribute__((aligned(16))) int8_t tile[kQw][kQw + 16];
     const int64_t e = blockIdx.y;
     const int n0 = blockIdx.x * kQw;
     const int c = (threadIdx.x & 7) * 8, kr = threadIdx.x >> 3;   // eight channels, one of 32 k rows
