@@ -424,7 +424,8 @@ class LayerFew:
         given = dict(Wr=Wr, bias=bias, sel_bias=sel_bias, W2=W2, s1=s1, s2=s2, Ws1=Ws1, Ws2=Ws2, ss1=ss1, ss2=ss2)
         for name, t in given.items():
             _sizes(t is None or tuple(t.shape) == tuple(want[name]), name)
-        if (s2 is None) == i8 or any((t is None) != (Fs == 0) for t in ((Ws1, Ws2, ss1, ss2) if i8 else (Ws1, Ws2))):
+        if ((s2 is None) == i8 or any((t is None) != (Fs == 0) for t in (Ws1, Ws2))
+                or any((t is None) != (Fs == 0 or not i8) for t in (ss1, ss2))):
             raise ValueError("weights and scales must be given together")
         if sel_bias is not None and score != "sigmoid":
             raise ValueError("sel_bias goes with sigmoid scores")
