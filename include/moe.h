@@ -28,8 +28,9 @@
  *   - Work is enqueued on `stream` (NULL = the null stream) and the call
  *     returns at once.  Arguments are validated synchronously before any
  *     launch; on a validation error nothing is enqueued.
- *   - Outputs must not alias inputs.  Results are deterministic: the same
- *     inputs give bit-identical outputs on every call.
+ *   - Outputs must not alias inputs, unless the entry point says so.  Results
+ *     are deterministic: the same inputs give bit-identical outputs on every
+ *     call.
  *   - S == 0 (or R == 0) is valid and enqueues nothing.
  *   - Every entry point enqueues kernels only (no allocation, copy, memset or
  *     host synchronisation), so a call made while `stream` is being captured
@@ -680,6 +681,7 @@ size_t moe_layer_few_workspace_bytes(const moe_layer_few_args* a);
  * to bf16 and quantised as in moe_grouped_ffn_i8.  The logits' last bits may differ
  * from moe_router_logits'.
  * With 8-bit weights D, F and Fs are multiples of 16.
+ * y may overlap x: the one launch that writes y comes after every read of x.
  * Errors: MOE_ERR_SHAPE for sizes (S > MOE_FEW_MAX_TOKENS among them), unknown modes,
  * sel_bias with softmax scores, and shared weights or scales where there are none to
  * be; otherwise as moe_layer_fwd. */

@@ -457,6 +457,7 @@ __global__ __launch_bounds__(kFewThreads) void few_quant_kernel(FewRows routed, 
     }
 }
 
+// The only launch that writes y, and no later one reads x: callers may let them overlap.
 // Sixty-four groups of four columns a workgroup; a wave takes every fourth expert of
 // the token's K, so that at most eight loads follow each other, and the waves' sums are
 // added in order.

@@ -391,3 +391,38 @@ def test_hidden_values_at_the_end_of_the_range():
     y = layer.LayerFew(2, torch.zeros((D, 1), device=DEV), W1.to(BF16), W2.to(BF16), 1)(x.to(BF16))["y"]
     assert float(y[0, 0]) == 2.0 ** 28 and not bool(y[0, 1:].any())
     assert float(y[1, 1]) == float("inf")
+
+
+@pytest.mark.parametrize("S", [8, 32, 64])
+@pytest.mark.parametrize("weights", ["bf16", "i8"])
+def test_shared_expert_past_the_last_level_cache(weights, S):
+    """Routed weights over 256 MB beside a shared expert whose own need not start on cache
+    lines; experts that most tokens pick, so that 16, 32 and 64 rows stage their weights."""
+    m = Model(2048, 80, 10, 1024, 1040, "sigmoid", weights, seed=15, bias_std=2.0)
+    x = m.tokens(S)
+    out = m.layer(S)(x)
+    most = int(torch.bincount(out["topk_idx"].reshape(-1).long(), minlength=80).max())
+    assert most > {8: 0, 32: 16, 64: 32}[S]
+    (check_i8 if weights == "i8" else check_bf16)(m, x, out)
+
+
+@pytest.mark.parametrize("weights", ["bf16", "i8"])
+def test_rows_of_an_experts_weights_off_the_cache_lines(weights):
+    """Rows that start on cache lines in one product and between them in the other (8 bits)."""
+    m = Model(2048, 80, 10, 1088, 1040, weights=weights, seed=16, bias_std=2.0)
+    x = m.tokens(48)
+    (check_i8 if weights == "i8" else check_bf16)(m, x, m.layer(48)(x))
+
+
+@pytest.mark.parametrize("weights", ["bf16", "i8"])
+def test_output_over_the_tokens_it_came_from(weights):
+    """y may be written over x, whole or shifted by rows."""
+    m = Model(272, 12, 3, 176, 64, weights=weights, seed=17)
+    lf = m.layer(6)
+    x = m.tokens(6)
+    first = lf(x)["y"].clone()
+    for rows in (slice(1, 6), slice(2, 4), slice(0, 6)):
+        ref = {k: v.clone() for k, v in m.layer(6)(first[rows].clone()).items()}
+        lf(x)
+        for k, v in lf(lf.out["y"][rows]).items():
+            assert torch.equal(v, ref[k]), (rows, k)
