@@ -59,7 +59,12 @@
 extern "C" {
 #endif
 
+/* The version changes when an entry point, a struct or a meaning does; the minor
+ * number rises when entry points are added to a version (1: 8-bit weights, and the
+ * layer for few tokens).  A consumer needs its own version and at least its own
+ * minor number. */
 #define MOE_ABI_VERSION 5
+#define MOE_ABI_MINOR 1
 
 typedef uint16_t moe_bf16; /* bit pattern of a bfloat16 value (b_x = 2 bytes) */
 
@@ -75,6 +80,10 @@ typedef enum {
 
 /* ABI version of the loaded library (MOE_ABI_VERSION at build time). */
 int moe_abi_version(void);
+
+/* Minor number of the loaded library (MOE_ABI_MINOR at build time); libraries of
+ * minor 0 have no such function. */
+int moe_abi_minor(void);
 
 /* Static, human-readable text for a moe_status value. Never NULL. */
 const char* moe_status_string(int status);

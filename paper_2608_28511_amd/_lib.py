@@ -83,6 +83,7 @@ U8 = torch.uint8
 
 _PROTOS = {
     "moe_abi_version": (C.c_int, []),
+    "moe_abi_minor": (C.c_int, []),
     "moe_status_string": (C.c_char_p, [C.c_int]),
     "moe_payload_bytes": (C.c_uint64, [i64, i32, i32]),
     "moe_router_logits_workspace_bytes": (sz, [i32, i32]),
@@ -139,6 +140,7 @@ _PROTOS = {
 }
 
 EXPORTED = tuple(_PROTOS)
+ABI = (5, 1)   # MOE_ABI_VERSION and MOE_ABI_MINOR that the prototypes are of
 
 
 def load(build_if_missing: bool = False) -> C.CDLL:
@@ -153,6 +155,10 @@ def load(build_if_missing: bool = False) -> C.CDLL:
         from . import build as _build
         _build.build()
     lib = C.CDLL(str(LIB_PATH))
+    have = (lib.moe_abi_version(), lib.moe_abi_minor() if hasattr(lib, "moe_abi_minor") else 0)
+    if have[0] != ABI[0] or have[1] < ABI[1]:
+        raise RuntimeError(f"{LIB_PATH} has ABI {have[0]}.{have[1]}, the binding needs {ABI[0]}.{ABI[1]}; "
+                           "run __graft_entry__.build()")
     for name, (res, args) in _PROTOS.items():
         f = getattr(lib, name)
         f.restype = res
@@ -207,6 +213,10 @@ BF16, F32, I32, I8 = torch.bfloat16, torch.float32, torch.int32, torch.int8
 
 def moe_abi_version() -> int:
     return load().moe_abi_version()
+
+
+def moe_abi_minor() -> int:
+    return load().moe_abi_minor()
 
 
 def moe_status_string(status: int) -> str:

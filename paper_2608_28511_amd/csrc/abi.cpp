@@ -87,6 +87,8 @@ extern "C" {
 
 int moe_abi_version(void) { return MOE_ABI_VERSION; }
 
+int moe_abi_minor(void) { return MOE_ABI_MINOR; }
+
 const char* moe_status_string(int status) {
     switch (status) {
         case MOE_OK: return "ok";
