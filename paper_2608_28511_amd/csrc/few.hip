@@ -96,8 +96,8 @@ __device__ __forceinline__ uint32_t wave_max_code(uint32_t v) {
 // largest of the lanes' tops bounds the K-th largest code from below, so only codes from
 // there on can be picked (at least K of them, since at least K lanes hold an expert: EPL
 // is the least power of two with 64 EPL >= E, and K <= 32).  They are gathered in LDS, one
-// a lane, and each counts those before it: no chain of K rounds (3 tokens, 512 experts
-// top-22: 10.0 -> 6.5 us, the sums of the logits included).
+// a lane, and each counts those before it: no chain of K rounds, which took half as long
+// again (3 tokens, 512 experts top-22: 7.6 us the launch, the sums of the logits included).
 template <int EPL>
 __device__ __forceinline__ void few_pick(const uint32_t (&code)[EPL], uint32_t top, int K, uint32_t* codes, uint2* cand,
                                          int& my_e, uint32_t& my_c) {
@@ -382,7 +382,8 @@ __global__ __launch_bounds__(kTableThreads) void few_table_kernel(const int32_t*
 }
 
 // At most 16 MBMAX tokens, and so rows an expert.  The fewer, the more waves a SIMD has registers for: 32
-// tokens of 8-bit weights top-16 of 256 122 us at four, 142 at the two that 64 leave; bf16 weights 215 / 217.
+// tokens of 8-bit weights top-16 of 256 experts of 1,024 x 1,536 122 us at four, 143 at the two that 64 leave,
+// top-6 of 64 of 2,048 x 1,024 71.0 / 77.2.
 constexpr int few_waves(int mb_max, int wave_lds) { return mb_max == 4 ? 2 : wave_lds * mb_max <= 8192 ? 4 : 3; }
 template <class T, int MBMAX>
 __global__ __launch_bounds__(kFewThreads, few_waves(MBMAX, T::kWaveLds)) void few_gemm_kernel(FewGemmArgs p) {
@@ -513,10 +514,11 @@ struct FewPlan {
 // Waves of a workgroup's four that share a slab's contraction, each keeping a step.  Four
 // give the most workgroups, which the CUs then share evenly, two the fewer that have to find
 // their rows and join their sums: two where they still make two workgroups a CU of more than
-// 16 tokens (us with 2 / 4: 64 tokens top-6 of 64 experts 121 / 129, top-22 of 512 422 / 440 and in 8
-// bits 251 / 280, but top-2 of 8 88 / 78), and with up to 16 tokens and bf16 weights eight a CU
-// (16 tokens top-8 of 256 349 / 361; 8 tokens of the 192-expert layer 354 / 347, one product's
-// choice varied; 1 token of 64 31 / 26.5; 16 tokens top-8 of 256 in 8 bits 193 / 189).
+// 16 tokens (us with 2 / 4: 64 tokens top-6 of 64 experts of 2,048 x 1,024 112 / 123 and in 8 bits
+// 79.8 / 85.3, top-22 of 512 of 672 x 1,856 416 / 440 and 255 / 276, but top-2 of 8 of 2,048 x 1,024
+// 47.2 / 37.2 and 35.0 / 32.4), and with up to 16 tokens and bf16 weights eight a CU (16 tokens
+// top-8 of 256 of 2,048 x 2,688 316 / 325; 8 tokens of the 192-expert layer 293 / 291; 1 token of 64
+// 34.2 / 27.2, 16 of them 89.1 / 91.4; in 8 bits 16 tokens top-8 of 256 170 / 166, 8 of 192 175 / 168).
 int few_share(bool i8, bool many, int slabs, int steps) {
     const int groups = many ? 2 : i8 ? 1 << 20 : 8;   // a CU's
     int wk = slabs / 2 >= (int64_t)groups * cu_count() ? 2 : 4;
@@ -525,17 +527,24 @@ int few_share(bool i8, bool many, int slabs, int steps) {
 }
 
 // Whether a launch of its own (2.5 us) finds the picked experts' rows, instead of every
-// workgroup of both products.  64 tokens top-22 of 512 422 us against 459 and, in 8 bits, 251
-// against 330; 40 tokens top-22 of 64 51 / 54; 64 tokens top-6 of 64 (384 picks) 121 / 121; 16 tokens
-// top-8 of 256 (128 picks) 349 / 348.
+// workgroup of both products.  64 tokens top-22 of 512 of 672 x 1,856 416 us against 452 and, in 8
+// bits, 255 against 339; 40 tokens top-22 of 64 of them 101 / 108 and 71.7 / 78.6; 64 tokens top-6 of 64
+// of 2,048 x 1,024 (384 picks) 112 / 112 and 80.2 / 85.4; 16 tokens top-8 of 256 (128 picks) 318 / 316 and
+// 167 / 166; 1 token of 64 30.2 / 27.1.
 bool few_table_pays(int picks) { return picks > kFewSearch; }
 
 // Columns of a slab.  8-bit weights take 32, or, where more than 16 tokens give an expert
-// several rows, 64, which halves how often they are read (us with 32 / 64: 64 tokens top-6 of
-// 64 81 / 77, top-2 of 8 57 / 53; top-22 of 512 251 / 267; 16 tokens top-8 of 256 189 / 192).
+// twelve rows or more on average, 64, which halves how often the rows are read, if that still
+// makes a workgroup a CU.  Of 53 calls of 17 to 64 tokens (4 to 512 experts, 512 to 2,816 by 512 to
+// 3,456) the 7 that take 64 take 0.91 to 1.02 of their time with 32, and of the others 36 of
+// 46 would lose up to a fifth (us with 32 / 64: 54 tokens top-10 of 22 of 2,560 x 1,408 81.3 /
+// 74.3, 30 top-22 of 39 of 2,176 x 2,688 115.5 / 110.4, 40 top-22 of 64 of 672 x 1,856 70.2 /
+// 71.7; 64 top-6 of 48 of 2,048 x 1,024 65.5 / 73.9, 33 top-4 of 4 of 1,664 x 1,920 34.5 / 40.8,
+// 64 top-22 of 512 of 672 x 1,856 254 / 267).
 int few_cols(const moe_layer_few_args* a) {
     if (a->weights != MOE_WEIGHTS_I8) return kSlabBf16;
-    return a->S > 16 && a->S * a->K >= 4 * (int64_t)a->E ? 2 * kSlabI8 : kSlabI8;
+    const int64_t slabs = (int64_t)a->E * cdiv(std::min(a->D, a->F), 2 * kSlabI8);   // all experts have rows
+    return a->S > 16 && a->S * a->K >= 12 * (int64_t)a->E && slabs >= cu_count() ? 2 * kSlabI8 : kSlabI8;
 }
 
 FewPlan few_plan_of(const moe_layer_few_args* a) {

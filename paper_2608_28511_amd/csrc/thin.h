@@ -302,10 +302,14 @@ __device__ __forceinline__ void thin_body(const ThinArgs& s, int n0, int kk, int
 // Whether weights [rows, row_bytes] at W, of which a call reads `bytes` in all, are better
 // read non-temporally: not what the last-level cache (256 MB) may still hold from the call
 // before, and not where rows do not start on cache lines, parts of which such loads fetch
-// twice (us, without / with the hint, bf16: 64 tokens of 64 experts, 537 MB, 119 / 105; 8 of the
-// 192-expert layer, 2.1 GB, 320 / 289; 1 token of 64, 50 MB, 25.5 / 29.5; 1 token top-22 of 512,
-// 110 MB, 39 / 41; 64 tokens top-22 of 512, rows of 1,344 bytes among them, 423 / 431 and, those
-// excepted, 403).
+// twice.  us, without / with the hint, each call on other weights than the one before, bf16: 64
+// tokens of 64 experts of 2,048 x 1,024, 537 MB, 124 / 112; 8 of the 192-expert layer, 2.1 GB, 318 /
+// 291; 64 tokens top-22 of 512, rows of 1,344 bytes among them, 437 / 445 and, those excepted, 416;
+// 8 bits: 32 tokens top-16 of 256 of 1,024 x 1,536 142 / 124; 16 tokens top-8 of 256 of 2,048 x
+// 2,688, 187 / 166.  Smaller calls may gain too where no call repeats the weights of the one before, and
+// may lose where it does: bf16 4 tokens of 64 experts, 200 MB at most, 58.5 / 54.0 and 45.1 / 51.6 repeated;
+// 1 token, 50 MB, 27.9 / 29.8 and 27.0 / 29.4; 8 bits 64 tokens of 64 experts, 256 MiB, 80.2 / 75.2
+// and 76.3 / 74.0, of 48 65.7 / 67.5 and 60.1 / 65.1.
 inline bool thin_nt(const void* W, int64_t row_bytes, int64_t bytes) {
     return bytes > (int64_t)256 << 20 && row_bytes % 128 == 0 && (uintptr_t)W % 128 == 0;
 }

@@ -170,11 +170,14 @@ __global__ __launch_bounds__(kThinThreads, NB == 2 ? 4 : 3) void rows_thin_kerne
     thin_rows<T, 2>(a, n0, few ? wave : 0, few ? 4 : 1, n, [](int i) { return i; }, [](int i) { return i; }, lds);
 }
 
-// Up to 20 rows an expert on average.  90 random expert FFNs (8 to 256 experts, 256 to 2,688 by 512 to 3,712, even
-// and Zipf loads) take of the tiles' time, by rows an expert: 4 to 8 0.65, 8 to 12 0.77, 12 to 16 0.81, 16 to
-// 20 0.85 (of single ones at most 0.99), 20 to 24 0.89 (1.04).  In us, tiles / this, even loads of 8 rows: 128 experts
-// of 2,048 x 1,024 117 / 103; 24 of 2,688 x 3,520 129 / 91; 8 of 512 x 1,024 21.3 / 13.4; and the other way, 3,001 rows
-// among those 128 by Zipf(1.1) 141 / 157, all 2,048 rows with one of 256 experts of 1,024 x 1,024 33 / 40.
+// Up to 20 rows an expert on average, whose loads the host does not know.  90 random expert FFNs (8 to 256 experts,
+// 256 to 2,688 by 512 to 3,712, even and Zipf(0.7) loads) take of the tiles' time, by rows an expert: 4 to 8 0.65, 8 to
+// 12 0.77, 12 to 16 0.81, 16 to 20 0.85 (of the drawn ones at most 0.99), 20 to 24 0.89 (1.04).  In us, tiles / this, even
+// loads of 8 rows: 128 experts of 2,048 x 1,024 119 / 104, 1,024 of them 803 / 743; 24 of 2,688 x 3,520 129 / 91; 8 of 512 x
+// 1,024 21.3 / 13.4.  An expert with many rows costs: its weights are read again for every 32 of them, and they for every
+// slab.  16 rows an expert by Zipf(1.1): 128 experts 141 / 131, 256 226 / 240, 1,024 804 / 877; half of 20 rows an expert
+// with one (two picks a token): 128 143 / 129, 1,024 892 / 913; all of them (one pick a token): 64 40 / 66, 256 58 / 108,
+// 1,024 142 / 368.
 bool rows_thin_pays(int E, int64_t R) { return R <= 20 * (int64_t)E; }
 
 // Columns of a slab.  64 read the rows half as often as 32, which pays where there are more than 12 an expert, unless

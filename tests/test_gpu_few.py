@@ -426,3 +426,14 @@ def test_output_over_the_tokens_it_came_from(weights):
         lf(x)
         for k, v in lf(lf.out["y"][rows]).items():
             assert torch.equal(v, ref[k]), (rows, k)
+
+
+@pytest.mark.parametrize("S, D, F, E, K, Fs", [(24, 1024, 1024, 16, 8, 0), (32, 1040, 1072, 24, 9, 80), (40, 1040, 1072, 24, 8, 80),
+                                               (64, 1024, 1040, 17, 16, 0), (32, 2048, 2688, 26, 10, 0),
+                                               (48, 2048, 2688, 26, 10, 144)])
+def test_wide_slabs_of_many_rows_an_expert(S, D, F, E, K, Fs):
+    """8-bit weights, twelve rows an expert or more, within and past the last-level cache."""
+    assert S * K >= 12 * E
+    m = Model(D, E, K, F, Fs, weights="i8", seed=S + E)
+    x = m.tokens(S)
+    check_i8(m, x, m.layer(S)(x))
