@@ -268,8 +268,9 @@ __device__ __forceinline__ void thin_body(const ThinArgs& s, int n0, int kk, int
                 f32x4 rest;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const float first = __uint_as_float(__float_as_uint(t[q]) & 0xffff0000u);
-                    rest[q] = fmaxf(t[q] - first, 0.f);   // an infinity or a NaN leaves none
+                    const uint32_t below = __builtin_elementwise_sub_sat(__float_as_uint(t[q]), 1u);
+                    const float first = __uint_as_float(below & 0xffff0000u);
+                    rest[q] = t[q] - first;
                     t[q] = first;
                 }
                 *(u32x2_thin*)(o + 8) = u32x2_thin{pack_bf16x2(rest[0], rest[1]), pack_bf16x2(rest[2], rest[3])};

@@ -437,3 +437,42 @@ def test_wide_slabs_of_many_rows_an_expert(S, D, F, E, K, Fs):
     m = Model(D, E, K, F, Fs, weights="i8", seed=S + E)
     x = m.tokens(S)
     check_i8(m, x, m.layer(S)(x))
+
+
+def test_infinite_weights():
+    """They give infinities, and NaN only where a hidden value is 0 or infinities of both signs meet."""
+    D, F = 32, 24
+    m = Model(D, 1, 1, F, seed=18)
+    x = m.tokens(20)
+    m.W1[0, :, 0] = 0.0                                            # h = 0
+    x[:, 0], m.W1[0, :, 1] = 1.0, 0.0
+    m.W1[0, 0, 1], m.W1[0, 0, 2] = 1.0, 0.75                       # h = 1: one part holds it
+    for f, d, sign in ((0, 0, 1), (1, 1, 1), (2, 2, -1), (3, 3, 1), (1, 4, 1), (2, 4, -1)):
+        m.W2[0, f, d] = sign * float("inf")
+    y = np64(m.layer(20)(x)["y"])
+    with np.errstate(invalid="ignore"):
+        h = np.maximum(np64(x) @ np64(m.W1[0]), 0.0) ** 2
+        terms = h[:, :, None] * np64(m.W2[0])
+        ref = terms.sum(1)
+    odd = ~np.isfinite(ref)
+    assert np.isnan(ref[:, 0]).all() and (ref[:, 1] == np.inf).all() and (h[:, 3] > 2.0 ** -20).any()
+    clear = (h[:, 3] == 0) | (h[:, 3] > 2.0 ** -20)                # elsewhere its sign hangs on a rounding
+    assert np.array_equal(y[clear][odd[clear]], ref[clear][odd[clear]], equal_nan=True)
+    assert np.isfinite(y[clear][~odd[clear]]).all()
+
+
+@pytest.mark.parametrize("e", [-100, -110, -118, -122, -126])
+def test_small_hidden_values(e):
+    """Hidden values down to the smallest normal number: their second parts are subnormal."""
+    D = F = 16
+    W1, W2 = torch.zeros((1, D, F), device=DEV), torch.zeros((1, F, D), device=DEV)
+    W1[0, 0, 0] = W1[0, 1, 0] = 1.0
+    W2[0, 0, 0] = 2.0 ** 100
+    x = torch.zeros((3, D), device=DEV)
+    x[0, 0], x[0, 1] = 2.0 ** (e // 2), 2.0 ** (e // 2 - 9)       # h = 2^e (1 + 2^-9)^2
+    x[1, 0] = 2.0 ** (e // 2)                                     # h = 2^e
+    x[2, 0], x[2, 1] = 2.0 ** (e // 2), 2.0 ** (e // 2 - 3)       # h = 2^e (1 + 2^-2 + 2^-6), a bf16 value
+    y = layer.LayerFew(3, torch.zeros((D, 1), device=DEV), W1.to(BF16), W2.to(BF16), 1)(x.to(BF16))["y"].double()
+    # 1 + 2^-8 + 2^-18 is 2^-18 from the middle of the bf16 values 1 and 1 + 2^-7, and h is held to 2^-16: either is right
+    assert float(y[0, 0]) in (2.0 ** (e + 100), 2.0 ** (e + 100) * (1 + 2.0 ** -7))
+    assert float(y[1, 0]) == 2.0 ** (e + 100) and float(y[2, 0]) == 2.0 ** (e + 100) * (1 + 2.0 ** -2 + 2.0 ** -6)
