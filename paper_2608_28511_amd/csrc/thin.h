@@ -101,10 +101,10 @@ struct ThinBf16 {
 // 8-bit weights, K-contiguous: slabs of 16 NB columns, steps of 128 k.  A fragment is 16
 // bytes of each of 16 channels and four places: loaded as such, an instruction takes half of
 // 16 cache lines.  NT: it takes eight whole ones, non-temporally, which the wave turns into
-// fragments in 2 NB KB of LDS of its own (row layout of tile_dma.h).  Half lines were fetched
-// twice non-temporally (16 tokens top-8 of 256: 185 us as they lie in memory, 204 with the
-// hint, 164 with whole lines and the hint), and whole lines alone cost the turn (3 tokens
-// top-22 of 512: 53 / 59).  Two steps ahead: three cost a workgroup a CU (53 / 55.5).
+// fragments in 2 NB KB of LDS of its own (row layout of tile_dma.h).  Half lines ask for each
+// line twice (16 tokens top-8 of 256: 188 us as they lie in memory, 202 with the hint, 166 with
+// whole lines and the hint; from memory come 0.50 GB a product in all three, 0.495 of them
+// weights), and whole lines alone cost the turn (3 tokens top-22 of 512: 53 / 59).  Two steps ahead: three cost a workgroup a CU (53 / 55.5).
 template <int NB, bool NT>
 struct ThinI8 {
     static constexpr bool kI8 = true;
@@ -263,7 +263,9 @@ __device__ __forceinline__ void thin_body(const ThinArgs& s, int n0, int kk, int
             }
             uint16_t* o = (uint16_t*)s.out + at;
             if constexpr (!T::kI8) {
-                // the value's first eight bits, and the rest rounded to as many: within 2^-16 of it
+                // The largest bf16 below the value, and the rest rounded to eight bits: within 2^-16 of it.
+                // Neither part of a positive value is zero, so an infinite weight makes no NaN of it,
+                // and an infinity is the largest bf16 and an infinity.
                 o += at - (col & 4);
                 f32x4 rest;
 #pragma unroll
@@ -302,8 +304,9 @@ __device__ __forceinline__ void thin_body(const ThinArgs& s, int n0, int kk, int
 
 // Whether weights [rows, row_bytes] at W, of which a call reads `bytes` in all, are better
 // read non-temporally: not what the last-level cache (256 MB) may still hold from the call
-// before, and not where rows do not start on cache lines, parts of which such loads fetch
-// twice.  us, without / with the hint, each call on other weights than the one before, bf16: 64
+// before, and not where rows do not start on cache lines, more of which are then read again
+// (64 tokens top-22 of 512, rows of 1,344 bytes in bf16: 1.48 GB from memory for 1.09 of weights,
+// with the hint 1.60; both products in 8 bits 1.14 / 1.33 for 1.09).  us, without / with the hint, each call on other weights than the one before, bf16: 64
 // tokens of 64 experts of 2,048 x 1,024, 537 MB, 124 / 112; 8 of the 192-expert layer, 2.1 GB, 318 /
 // 291; 64 tokens top-22 of 512, rows of 1,344 bytes among them, 437 / 445 and, those excepted, 416;
 // 8 bits: 32 tokens top-16 of 256 of 1,024 x 1,536 142 / 124; 16 tokens top-8 of 256 of 2,048 x

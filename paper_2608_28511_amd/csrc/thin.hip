@@ -94,7 +94,7 @@ __global__ __launch_bounds__(kProjWaves * 64) void proj_few_kernel(const uint16_
 #pragma unroll
     for (int v = 0; v < kPieces; ++v) sum(wave, v) = acc[v / NB][v % NB];
     __syncthreads();
-        for (int v = kk; v < kPieces; v += WK) {
+    for (int v = kk; v < kPieces; v += WK) {
         const int r = 16 * (v / NB) + (lane & 15), col = n0 + T::piece_col(v % NB, lane);
         if (r >= M || col >= s.N) continue;   // N is a multiple of 8
         f32x4 t = sum(slab * WK, v);

@@ -346,3 +346,11 @@ def test_refusals_on_the_device():
         layer.grouped_ffn_i8(x.float(), off, W1q, s1, W2q, s2)
     with pytest.raises(L.MoeError):
         layer.quant_rows_i8(torch.zeros(2, 24, dtype=BF16, device=DEV))
+
+
+@pytest.mark.parametrize("E, Kd, N", [(64, 272, 104), (100, 1040, 40), (256, 128, 72)])
+def test_one_expert_with_every_row(E, Kd, N):
+    """The largest calls that are taken for few rows an expert, all of them with one."""
+    counts = [0] * E
+    counts[E // 3] = 20 * E
+    test_grouped_gemm_i8(counts, Kd, N, 1)
