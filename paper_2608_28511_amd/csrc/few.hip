@@ -19,9 +19,9 @@
 //   few_combine  y = bf16(sum_k p_k y_k + shared), all sums in fp32 and fixed order
 //
 // us of a call, and the time of its weights at the 6.16 TB/s of a large read: 1 token top-6 of 64
-// experts of 2,048 x 1,024 25 (8; launches 2.4 each), 64 tokens 105 (87), 8 tokens of the production
-// layer 265-293 (310), in 8 bits 16 tokens top-8 of 256 of 2,048 x 2,688 164-179 (183), 3 tokens top-22
-// of 512 of 672 x 1,856 54 (26).
+// experts of 2,048 x 1,024 25-28 (8; launches 2.4 each), 64 tokens 106-112 (87), 8 tokens of the
+// production layer 265-298 (310), in 8 bits 16 tokens top-8 of 256 of 2,048 x 2,688 164-179 (183), 3 tokens
+// top-22 of 512 of 672 x 1,856 53-61 (26).
 #include <algorithm>
 
 #include "kernels.h"
