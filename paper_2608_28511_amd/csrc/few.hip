@@ -661,6 +661,7 @@ hipError_t launch_layer_few(const moe_layer_few_args* a, hipStream_t st) {
                 cols == kSlabI8 ? go(few_gemm_kernel<ThinI8<2, NT>, 2>) : go(few_gemm_kernel<ThinI8<4, NT>, 2>);
             else cols == kSlabI8 ? go(few_gemm_kernel<ThinI8<2, NT>, 4>) : go(few_gemm_kernel<ThinI8<4, NT>, 4>);
         };
+        // the routed experts' weights decide for the shared one's, a small part of the call
         if (thin_nt(r.W, (int64_t)(i8 ? r.Kd : r.N) * wb, 2 * (int64_t)p.r_experts * r.w_bytes)) pick(std::true_type{});
         else pick(std::false_type{});
         return launch_check(st);

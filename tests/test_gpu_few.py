@@ -476,3 +476,25 @@ def test_small_hidden_values(e):
     # 1 + 2^-8 + 2^-18 is 2^-18 from the middle of the bf16 values 1 and 1 + 2^-7, and h is held to 2^-16: either is right
     assert float(y[0, 0]) in (2.0 ** (e + 100), 2.0 ** (e + 100) * (1 + 2.0 ** -7))
     assert float(y[1, 0]) == 2.0 ** (e + 100) and float(y[2, 0]) == 2.0 ** (e + 100) * (1 + 2.0 ** -2 + 2.0 ** -6)
+
+
+@pytest.mark.parametrize("weights", ["bf16", "i8"])
+@pytest.mark.parametrize("S, D, E, K, F, Fs", [(1, 64, 5, 2, 48, 0), (9, 272, 40, 7, 176, 80), (30, 144, 64, 12, 336, 16),
+                                               (64, 528, 24, 8, 112, 272)])
+def test_writes_its_buffers_only(S, D, E, K, F, Fs, weights):
+    """A call without exported picks and without biases, in a workspace of just the size it asks
+    for, among guard bytes; the workspace holds anything before."""
+    m = Model(D, E, K, F, Fs, weights=weights, seed=19)
+    x = m.tokens(S)
+    kw = {k: v for k, v in m.kw.items() if k not in ("bias", "sel_bias", "score")}
+    ref = {k: v.clone() for k, v in layer.LayerFew(S, m.Wr, m.w1, m.w2, K, **kw)(x).items()}
+    mode = L.WEIGHTS_I8 if weights == "i8" else L.WEIGHTS_BF16
+    n = L.moe_layer_few_workspace_bytes(L.layer_few_args(S, D, E, K, F, Fs, weights=mode))
+    for fill in (0xFF, 0x00, 0x7F):
+        ws = torch.full((n + 512,), fill, dtype=torch.uint8, device=DEV)
+        y = torch.full((S + 2, D), -3.0, dtype=BF16, device=DEV)
+        L.moe_layer_few(L.layer_few_args(S, D, E, K, F, Fs, weights=mode, ws=ws[256:256 + n], x=x, Wr=m.Wr, W1=m.w1,
+                                         W2=m.w2, y=y[1:-1], **kw))
+        assert torch.equal(y[1:-1], ref["y"])
+        assert bool((y[0] == -3).all()) and bool((y[-1] == -3).all())
+        assert bool((ws[:256] == fill).all()) and bool((ws[256 + n:] == fill).all())

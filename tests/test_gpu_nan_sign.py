@@ -109,3 +109,19 @@ def test_other_values_keep_their_bits():
     assert torch.equal(h[normal, 0], ref[normal].float().to(BF16))
     assert bool((h[~normal, 0].double() <= 2.0 ** -126).all()) and not bool(h[:, 1:].any())
     assert not bool((h.view(torch.int16) < 0).any())         # +0, never -0
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+def test_mx_payload(sign):
+    """A weight of the up projection that reads an MX-FP8 payload."""
+    R, D, F = 300, 256, 200
+    x, off, W1, _, _ = inputs(R, D, F)
+    order = torch.arange(R, dtype=torch.int32, device=DEV)
+    q, s = layer.dispatch_mxfp8(x, None, order, 1)[:2]
+    sched = layer.grouped_schedule(off, 2, R)
+    h0 = layer.grouped_gemm_mxfp8(q, s, sched, W1, 1)
+    W1[1, 3, F - 1] = bad(sign)[0]
+    h = layer.grouped_gemm_mxfp8(q, s, sched, W1, 1)
+    hit = torch.zeros((R, F), dtype=torch.bool, device=DEV)
+    hit[R // 3:, F - 1] = True
+    assert torch.equal(torch.isnan(h), hit) and torch.equal(h[~hit], h0[~hit])
